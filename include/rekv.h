@@ -10,8 +10,9 @@
  *     (Eq. 2 with tau = 1) and the r best frames' KV is reloaded onto the GPU
  *     (internal video KV-cache retrieval),
  *   - the question tokens attend to the retrieved KV and to themselves (Eq. 3).
- * This library is those steps for one attention layer on one GPU.  The Q/K/V
- * projections, RoPE and the rest of the model stay with the caller.
+ * This library is those steps for one attention layer on one GPU, and the same for many
+ * streams and users on one paged cache (rekv_append_kv and below).  The Q/K/V projections
+ * and the rest of the model stay with the caller; Q and K arrive positioned, by rekv_rotate if wanted.
  *
  * Conventions shared by every call
  *   - Pointers are DEVICE pointers unless a parameter says "host".
@@ -369,6 +370,110 @@ rekv_status rekv_offload_kv(rekv_ctx* ctx, const void* dev_k, const void* dev_v,
                             void* host_v, int64_t first_frame, int32_t n_frames, void* stream);
 rekv_status rekv_offload_wait(rekv_ctx* ctx);
 rekv_status rekv_offload_join(rekv_ctx* ctx, void* stream);
+
+/*
+ * Many streams and users on one paged KV cache.
+ *
+ * A page holds page_size tokens' keys (in k_pages) and values (in v_pages), each
+ * [n_pages, page_size, Hkv, D] in the context's dtype; page_size is free, and with
+ * page_size = N_f the pages are the frames that rekv_frame_keys, rekv_gather_kv and
+ * rekv_attention_indexed work on.  A batch has n_seqs sequences.  Sequence s owns the
+ * tokens [token_start[s], token_start[s + 1]) of the batch's n_tokens token rows, n_s of
+ * them (none at all is fine); they are the newest of its kv_len[s] tokens, so new token i
+ * has index kv_len[s] - n_s + i in its sequence.  Index j of a sequence lies in page
+ * page_table[s][j / page_size], row j % page_size.
+ *
+ *   token_start  device int32 [n_seqs + 1], not decreasing, from 0 to at most n_tokens
+ *   kv_len       device int32 [n_seqs], at most max_pages * page_size
+ *   page_table   device int32 [n_seqs, table_stride], the first max_pages of a row valid.
+ *                Only entries of pages that a call reads or writes matter: pages that
+ *                left the window may be given back (entry -1, or anything).
+ *
+ * Token rows from token_start[n_seqs] on (the padding of a captured step) are neither read
+ * for others nor written.  Lengths and tables are read on the device, so a captured call may
+ * be replayed with others.  What they say is never followed out of bounds: page numbers
+ * outside [0, n_pages) are taken as the nearest page when read and skipped when written.
+ * n_pages * page_size and max_pages * page_size are below 2^30; the arrays may be larger than 4 GiB.
+ */
+typedef struct {
+    void* k_pages;
+    void* v_pages;
+    const int32_t* token_start;
+    const int32_t* kv_len;
+    const int32_t* page_table;
+    int64_t table_stride;
+    int32_t max_pages, n_pages, page_size, n_seqs, n_tokens;
+} rekv_paged;
+
+/*
+ * Rotary positions with one or several axes.  Pair i of a head vector (0 <= i < D / 2) turns by
+ * position[axis of i] * base^(-2i / D).  Axis a owns sections[a] pairs; the sections add up to
+ * D / 2.  order 0: section after section; 1: the pairs go in turn to the axes that have
+ * pairs left (time, height, width, time, ...).  layout 0: pair i is (i, i + D / 2), 1: (2i, 2i + 1).
+ * inverse 1 turns back, which is also the gradient of a rotation.  Angles are formed in double precision.
+ */
+typedef struct {
+    double base;         /* 1 < base < 1e30 */
+    int32_t layout, order, inverse;
+    int32_t n_axes;      /* 1..4 */
+    int32_t sections[4];
+} rekv_rotary;
+
+/*
+ * Rotates n_tokens x n_heads head vectors.
+ *   x, out     [n_tokens, n_heads, D], tokens x_stride and out_stride elements apart (at least
+ *              n_heads * D, multiples of 16 bytes); out may be x itself with the same stride
+ *   positions  device int32 [n_axes, n_tokens], axes positions_stride (at least n_tokens) apart
+ */
+rekv_status rekv_rotate(rekv_ctx* ctx, const rekv_rotary* rotary, const void* x, int64_t x_stride,
+                        int32_t n_tokens, int32_t n_heads, const int32_t* positions, int64_t positions_stride,
+                        void* out, int64_t out_stride, void* stream);
+
+/*
+ * Appends the batch's new keys and values to their sequences' pages, the keys rotated on the way, and
+ * rotates the queries in the same pass.
+ *   k, v       [n_tokens, Hkv, D], tokens k_stride and v_stride elements apart
+ *   q, q_out   [n_tokens, Hq, D], tokens q_stride apart, q_out dense; both NULL: no queries; q_out may be q
+ *   rotary     NULL: keys (and queries) are taken as they are
+ *   positions  device int32 [n_axes, n_tokens]; NULL: a token's position is its index in its
+ *              sequence, on every axis
+ * kv_len counts the new tokens.  Tokens whose index lies outside the table's max_pages, or whose page
+ * is outside [0, n_pages), are not written.  Rows of q_out behind the last sequence stay as they were.
+ */
+rekv_status rekv_append_kv(rekv_ctx* ctx, const rekv_paged* cache, const rekv_rotary* rotary, const void* k,
+                           int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,
+                           void* q_out, const int32_t* positions, int64_t positions_stride, void* stream);
+
+/*
+ * Causal attention of a batch's new tokens over their sequences' pages, whole or through a sliding
+ * window beside the first tokens, which stay visible (sinks).  The token at index p sees index j iff
+ *   j <= p  and  (window < 0  or  p - j < window  or  j < sinks).
+ * A token that sees nothing (window 0 and no sinks, a negative index) gets zeros.
+ *   q, out     [n_tokens, Hq, D]; the new tokens' keys and values are already in the pages
+ *   window     tokens, the token itself among them; negative: no window (sinks is then without effect)
+ *   max_kv     about the largest kv_len, for the split of the work only: any value gives right results
+ *   workspace  device memory of at least the bytes that rekv_attention_paged_workspace gives for the same
+ *              sizes, 256-byte aligned, used by this call only until it has run; may be NULL where they are 0.
+ * The call allocates nothing and uses nothing of its context but the shape, so calls of one context on
+ * several streams, and captured ones, only need workspaces of their own.
+ */
+rekv_status rekv_attention_paged(rekv_ctx* ctx, const rekv_paged* cache, const void* q, int32_t max_kv,
+                                 int32_t window, int32_t sinks, void* out, void* workspace,
+                                 int64_t workspace_bytes, void* stream);
+
+/*
+ * The same for a batch that shares a long prefix, computed once for all its rows: every new token sees
+ * all n_prefix >= 1 tokens of the prefix and, causally, its own sequence's tokens.  kv_len, the
+ * indexes and page_table count the own tokens only.
+ *   prefix_pages  device int32 [ceil(n_prefix / page_size)], pages of the same cache
+ */
+rekv_status rekv_attention_shared_prefix(rekv_ctx* ctx, const rekv_paged* cache, const void* q,
+                                         const int32_t* prefix_pages, int32_t n_prefix, int32_t max_kv,
+                                         void* out, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Workspace of the two calls above (n_prefix 0: rekv_attention_paged), which depends on sizes alone.  Host call. */
+rekv_status rekv_attention_paged_workspace(rekv_ctx* ctx, int32_t n_tokens, int32_t n_seqs, int32_t max_kv,
+                                           int32_t window, int32_t sinks, int32_t n_prefix, int64_t* bytes);
 
 /*
  * Measurement probes.  They are not operations of the method: they show what this GPU

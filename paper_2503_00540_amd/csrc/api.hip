@@ -1,5 +1,6 @@
 // The C ABI of librekv: argument validation, the context (workspace, side stream, events)
 // and dispatch to the kernels.  No arithmetic of the method happens in this file.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -733,6 +734,191 @@ rekv_status rekv_offload_join(rekv_ctx* c, void* stream) {
     hipError_t e = hipEventRecord(c->ev_side, c->side);
     if (e == hipSuccess) e = hipStreamWaitEvent(static_cast<hipStream_t>(stream), c->ev_side, 0);
     return e == hipSuccess ? REKV_OK : fail_hip(c, "rekv_offload_join", e);
+}
+
+// ---- many streams and users on one paged cache
+
+// The checks that every call on a batch shares; the launch's form of the batch.
+static rekv_status paged_batch(rekv_ctx* c, const char* fn, const rekv_paged* in, rekv::PagedBatch* b) {
+    if (!in) return fail(c, REKV_ERR_INVALID_ARG, "%s: null pointer", fn);
+    if (in->n_pages <= 0 || in->page_size <= 0 || in->max_pages <= 0 || in->table_stride < in->max_pages || in->n_seqs <= 0 || in->n_tokens <= 0)
+        return fail(c, REKV_ERR_INVALID_ARG, "%s: n_pages=%d page_size=%d max_pages=%d table_stride=%lld n_seqs=%d n_tokens=%d", fn, in->n_pages,
+                    in->page_size, in->max_pages, (long long)in->table_stride, in->n_seqs, in->n_tokens);
+    if (!in->k_pages || !in->v_pages || !in->token_start || !in->kv_len || !in->page_table)
+        return fail(c, REKV_ERR_INVALID_ARG, "%s: null pointer", fn);
+    if (!aligned16(in->k_pages) || !aligned16(in->v_pages))
+        return fail(c, REKV_ERR_INVALID_ARG, "%s: pages must be 16-byte aligned", fn);
+    if ((int64_t)in->n_pages * in->page_size >= (1 << 30) || (int64_t)in->max_pages * in->page_size >= (1 << 30))
+        return fail(c, REKV_ERR_UNSUPPORTED, "%s: %d pages, %d of them per sequence, of %d tokens: below 2^30 tokens each", fn, in->n_pages,
+                    in->max_pages, in->page_size);
+    if ((int64_t)in->n_tokens * c->shape.n_q_heads >= (1 << 30) || in->n_seqs >= (1 << 24))
+        return fail(c, REKV_ERR_UNSUPPORTED, "%s: %d tokens of %d sequences are too many", fn, in->n_tokens, in->n_seqs);
+    b->k_pages = in->k_pages; b->v_pages = in->v_pages;
+    b->token_start = in->token_start; b->kv_len = in->kv_len; b->page_table = in->page_table; b->table_stride = in->table_stride;
+    b->max_pages = in->max_pages; b->n_pages = in->n_pages; b->n_seqs = in->n_seqs; b->n_tokens = in->n_tokens;
+    b->capacity = in->max_pages * in->page_size;
+    b->by_page = rekv::div31((uint32_t)in->page_size);
+    return REKV_OK;
+}
+
+// Kernels go to the current device, as the pointers do; a context of another one is a mistake.
+static rekv_status on_device(rekv_ctx* c, const char* fn) {
+    int device = -1;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return fail_hip(c, fn, e);
+    if (device != c->device)
+        return fail(c, REKV_ERR_INVALID_ARG, "%s: the context was created on device %d, the current one is %d", fn, c->device, device);
+    return REKV_OK;
+}
+
+static rekv_status rotary_args(rekv_ctx* c, const char* fn, const rekv_rotary* in, rekv::Rotary* r) {
+    const int d = c->shape.head_dim, epc = c->shape.dtype == REKV_BF16 ? 8 : 4, half = d / 2;
+    if (d > 2 * rekv::MAX_PAIRS || d % (2 * epc) != 0)
+        return fail(c, REKV_ERR_UNSUPPORTED, "%s: head_dim=%d must be a multiple of %d, at most %d", fn, d, 2 * epc, 2 * rekv::MAX_PAIRS);
+    memset(r, 0, sizeof(*r));
+    if (!in) return REKV_OK;
+    if (!(in->base > 1.0) || !(in->base < 1e30) || (in->layout != 0 && in->layout != 1) || (in->order != 0 && in->order != 1) ||
+        (in->inverse != 0 && in->inverse != 1) || in->n_axes < 1 || in->n_axes > rekv::MAX_AXES)
+        return fail(c, REKV_ERR_INVALID_ARG, "%s: base=%g (> 1) layout=%d order=%d inverse=%d (each 0 or 1) n_axes=%d (1..%d)", fn, in->base,
+                    in->layout, in->order, in->inverse, in->n_axes, rekv::MAX_AXES);
+    int64_t sum = 0;
+    for (int i = 0; i < in->n_axes; ++i) {
+        if (in->sections[i] < 0) return fail(c, REKV_ERR_INVALID_ARG, "%s: section %d has %d pairs", fn, i, in->sections[i]);
+        sum += in->sections[i];
+    }
+    if (sum != half) return fail(c, REKV_ERR_INVALID_ARG, "%s: the sections have %lld pairs, a head vector has %d", fn, (long long)sum, half);
+    int32_t left[rekv::MAX_AXES] = {};
+    for (int i = 0; i < in->n_axes; ++i) left[i] = in->sections[i];
+    for (int i = 0, a = 0; i < half; ++i) {
+        while (left[a] == 0) a = (a + 1) % in->n_axes;
+        r->axis[i] = (uint8_t)a;
+        --left[a];
+        if (in->order == 1) a = (a + 1) % in->n_axes;
+    }
+    // the frequencies as powers of one ratio, in extended precision
+    const long double ratio = powl((long double)in->base, -2.0L / d);
+    long double theta = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
+    if (in->inverse) theta = -theta;
+    for (int i = 0; i < half; ++i, theta *= ratio) r->turns[i] = (double)theta;
+    r->n_axes = in->n_axes;
+    r->interleaved = in->layout;
+    return REKV_OK;
+}
+
+rekv_status rekv_rotate(rekv_ctx* c, const rekv_rotary* rotary, const void* x, int64_t x_stride, int32_t n_tokens,
+                        int32_t n_heads, const int32_t* positions, int64_t positions_stride, void* out, int64_t out_stride,
+                        void* stream) {
+    if (!c) return REKV_ERR_INVALID_ARG;
+    if (!rotary || !x || !positions || !out) return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: null pointer");
+    if (n_tokens <= 0 || n_heads <= 0 || positions_stride < n_tokens)
+        return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: n_tokens=%d n_heads=%d positions_stride=%lld", n_tokens, n_heads, (long long)positions_stride);
+    rekv::RotateArgs a;
+    memset(&a, 0, sizeof(a));
+    rekv_status s = rotary_args(c, "rekv_rotate", rotary, &a.r);
+    if (s != REKV_OK) return s;
+    const int64_t row = (int64_t)n_heads * c->shape.head_dim, lane = 16 / (int64_t)elem_size(c);
+    if (!aligned16(x) || !aligned16(out) || x_stride < row || out_stride < row || x_stride % lane != 0 || out_stride % lane != 0)
+        return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: x and out must be 16-byte aligned, x_stride=%lld and out_stride=%lld multiples of %lld of at least %lld",
+                    (long long)x_stride, (long long)out_stride, (long long)lane, (long long)row);
+    if (x == out && x_stride != out_stride) return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: in place with strides %lld and %lld",
+                                                        (long long)x_stride, (long long)out_stride);
+    s = on_device(c, "rekv_rotate");
+    if (s != REKV_OK) return s;
+    a.positions = positions; a.positions_stride = positions_stride;
+    a.n_tokens = n_tokens; a.head_dim = c->shape.head_dim; a.n_q_heads = n_heads;
+    a.q = x; a.q_out = out; a.q_stride = x_stride; a.q_out_stride = out_stride;
+    hipError_t e = rekv::rotate_launch(a, c->shape.dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? REKV_OK : fail_hip(c, "rekv_rotate", e);
+}
+
+rekv_status rekv_append_kv(rekv_ctx* c, const rekv_paged* cache, const rekv_rotary* rotary, const void* k, int64_t k_stride,
+                           const void* v, int64_t v_stride, const void* q, int64_t q_stride, void* q_out, const int32_t* positions,
+                           int64_t positions_stride, void* stream) {
+    if (!c) return REKV_ERR_INVALID_ARG;
+    if (!k || !v || !q != !q_out) return fail(c, REKV_ERR_INVALID_ARG, "rekv_append_kv: null pointer");
+    rekv::RotateArgs a;
+    memset(&a, 0, sizeof(a));
+    rekv_status s = paged_batch(c, "rekv_append_kv", cache, &a.b);
+    if (s == REKV_OK) s = rotary_args(c, "rekv_append_kv", rotary, &a.r);
+    if (s != REKV_OK) return s;
+    if (positions && positions_stride < cache->n_tokens)
+        return fail(c, REKV_ERR_INVALID_ARG, "rekv_append_kv: positions_stride=%lld for %d tokens", (long long)positions_stride, cache->n_tokens);
+    const int64_t d = c->shape.head_dim, kv_row = c->shape.n_kv_heads * d, q_row = c->shape.n_q_heads * d, lane = 16 / (int64_t)elem_size(c);
+    if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || k_stride < kv_row || v_stride < kv_row || (q && q_stride < q_row) ||
+        k_stride % lane != 0 || v_stride % lane != 0 || (q && q_stride % lane != 0))
+        return fail(c, REKV_ERR_INVALID_ARG, "rekv_append_kv: k, v, q and q_out must be 16-byte aligned, k_stride=%lld, v_stride=%lld and q_stride=%lld "
+                    "multiples of %lld of at least a token's heads", (long long)k_stride, (long long)v_stride, (long long)q_stride, (long long)lane);
+    if (q && q == q_out && q_stride != q_row) return fail(c, REKV_ERR_INVALID_ARG, "rekv_append_kv: q_out is dense, q has stride %lld", (long long)q_stride);
+    s = on_device(c, "rekv_append_kv");
+    if (s != REKV_OK) return s;
+    a.positions = positions; a.positions_stride = positions_stride;
+    a.n_tokens = cache->n_tokens; a.head_dim = c->shape.head_dim; a.n_q_heads = c->shape.n_q_heads; a.n_kv_heads = c->shape.n_kv_heads;
+    a.q = q; a.q_out = q_out; a.q_stride = q_stride; a.q_out_stride = q_row;
+    a.k = k; a.v = v; a.k_stride = k_stride; a.v_stride = v_stride;
+    hipError_t e = rekv::rotate_launch(a, c->shape.dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? REKV_OK : fail_hip(c, "rekv_append_kv", e);
+}
+
+constexpr int32_t MOST_KEYS = 1 << 30;       // no sequence is longer: a larger window is none
+
+static rekv::PagedPlan paged_plan(rekv_ctx* c, int64_t n_tokens, int64_t n_seqs, int32_t max_kv, int32_t window, int32_t sinks, int64_t n_prefix) {
+    return rekv::attn_paged_plan(c->shape.dtype, c->shape.n_q_heads, c->shape.n_kv_heads, c->shape.head_dim, n_tokens, n_seqs,
+                                 max_kv < 1 ? 1 : max_kv < MOST_KEYS ? max_kv : MOST_KEYS, window < MOST_KEYS ? window : -1, sinks, n_prefix);
+}
+
+static rekv_status attention_paged(rekv_ctx* c, const char* fn, const rekv_paged* cache, const void* q, const int32_t* prefix_pages,
+                                   int32_t n_prefix, int32_t max_kv, int32_t window, int32_t sinks, void* out, void* workspace,
+                                   int64_t workspace_bytes, void* stream) {
+    if (!c) return REKV_ERR_INVALID_ARG;
+    if (!q || !out) return fail(c, REKV_ERR_INVALID_ARG, "%s: null pointer", fn);
+    if (!aligned16(q) || !aligned16(out)) return fail(c, REKV_ERR_INVALID_ARG, "%s: q and out must be 16-byte aligned", fn);
+    if (sinks < 0) return fail(c, REKV_ERR_INVALID_ARG, "%s: sinks=%d", fn, sinks);
+    rekv::PagedProblem p;
+    memset(&p, 0, sizeof(p));
+    rekv_status s = paged_batch(c, fn, cache, &p.b);
+    if (s != REKV_OK) return s;
+    const rekv::PagedPlan plan = paged_plan(c, cache->n_tokens, cache->n_seqs, max_kv, window, sinks, n_prefix);
+    if (plan.workspace_bytes > 0 && (!workspace || workspace_bytes < plan.workspace_bytes || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0))
+        return fail(c, REKV_ERR_INVALID_ARG, "%s: needs a 256-byte aligned workspace of %lld bytes, got %lld", fn, (long long)plan.workspace_bytes,
+                    workspace ? (long long)workspace_bytes : 0ll);
+    const int64_t jobs = ((int64_t)plan.prefix_blocks * plan.prefix_splits + (int64_t)plan.blocks * plan.splits) * c->shape.n_kv_heads;
+    if (jobs > 0x7FFFFFFF) return fail(c, REKV_ERR_UNSUPPORTED, "%s: grid of %lld workgroups", fn, (long long)jobs);
+    s = on_device(c, fn);
+    if (s != REKV_OK) return s;
+    p.q = q; p.out = out;
+    p.prefix_pages = prefix_pages; p.n_prefix = n_prefix;
+    p.window = window < MOST_KEYS ? window : -1; p.sinks = sinks;
+    p.n_q_heads = c->shape.n_q_heads; p.n_kv_heads = c->shape.n_kv_heads; p.head_dim = c->shape.head_dim; p.scale = c->scale;
+    hipError_t e = rekv::attn_paged_launch(p, plan, c->shape.dtype, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? REKV_OK : fail_hip(c, fn, e);
+}
+
+rekv_status rekv_attention_paged(rekv_ctx* c, const rekv_paged* cache, const void* q, int32_t max_kv, int32_t window, int32_t sinks,
+                                 void* out, void* workspace, int64_t workspace_bytes, void* stream) {
+    return attention_paged(c, "rekv_attention_paged", cache, q, nullptr, 0, max_kv, window, sinks, out, workspace, workspace_bytes, stream);
+}
+
+rekv_status rekv_attention_shared_prefix(rekv_ctx* c, const rekv_paged* cache, const void* q, const int32_t* prefix_pages,
+                                         int32_t n_prefix, int32_t max_kv, void* out, void* workspace, int64_t workspace_bytes,
+                                         void* stream) {
+    if (!c) return REKV_ERR_INVALID_ARG;
+    if (!prefix_pages) return fail(c, REKV_ERR_INVALID_ARG, "rekv_attention_shared_prefix: null pointer");
+    if (n_prefix <= 0 || n_prefix >= MOST_KEYS) return fail(c, REKV_ERR_INVALID_ARG, "rekv_attention_shared_prefix: n_prefix=%d (1 to 2^30 - 1)", n_prefix);
+    return attention_paged(c, "rekv_attention_shared_prefix", cache, q, prefix_pages, n_prefix, max_kv, -1, 0, out, workspace, workspace_bytes,
+                           stream);
+}
+
+rekv_status rekv_attention_paged_workspace(rekv_ctx* c, int32_t n_tokens, int32_t n_seqs, int32_t max_kv, int32_t window, int32_t sinks,
+                                           int32_t n_prefix, int64_t* bytes) {
+    if (!c) return REKV_ERR_INVALID_ARG;
+    if (!bytes) return fail(c, REKV_ERR_INVALID_ARG, "rekv_attention_paged_workspace: null pointer");
+    *bytes = 0;
+    if (n_tokens <= 0 || n_seqs <= 0 || n_seqs >= (1 << 24) || (int64_t)n_tokens * c->shape.n_q_heads >= (1 << 30) || sinks < 0 || n_prefix < 0 ||
+        n_prefix >= MOST_KEYS)
+        return fail(c, REKV_ERR_INVALID_ARG, "rekv_attention_paged_workspace: n_tokens=%d n_seqs=%d sinks=%d n_prefix=%d", n_tokens, n_seqs, sinks,
+                    n_prefix);
+    *bytes = paged_plan(c, n_tokens, n_seqs, max_kv, window, sinks, n_prefix).workspace_bytes;
+    return REKV_OK;
 }
 
 rekv_status rekv_probe_copy(rekv_ctx* c, void* dst, const void* src, int64_t n_bytes, void* stream) {

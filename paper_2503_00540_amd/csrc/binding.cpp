@@ -14,6 +14,7 @@
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
@@ -467,6 +468,182 @@ METHOD(decode_attention, 9) {    // q, k_ret, v_ret, k_text, v_text, n_text_toke
     return st ? raise_status(g.c, st) : out.take();
 }
 
+// ---- many streams and users on one paged cache
+
+bool here(const Tensor* t) { return t->is_cuda() && t->device().index() == c10::hip::current_device(); }
+
+// [tokens, heads, D] whose head vectors lie side by side (heads < 0: any number); the elements between tokens.
+const Tensor* token_rows(Args& g, PyObject* o, int64_t heads, int64_t* stride) {
+    const Tensor* t = g.tensor(o);
+    if (!t) return nullptr;
+    g.need(here(t) && t->scalar_type() == g.c->dtype && t->dim() == 3 && t->size(2) == g.c->d && (heads < 0 || t->size(1) == heads));
+    g.need(g.ok && t->stride(2) == 1 && (t->size(1) <= 1 || t->stride(1) == g.c->d) && Args::fits(t->size(0)) && Args::fits(t->size(1)));
+    if (!g.ok) return nullptr;
+    *stride = t->size(0) > 1 ? t->stride(0) : t->size(1) * t->size(2);
+    return t;
+}
+
+// sections, base, layout, order: the arguments a rotation needs
+struct Rotation {
+    rekv_rotary r;
+    Rotation(Args& g, PyObject* sections, PyObject* base, PyObject* layout, PyObject* order) : r{} {
+        r.base = g.f64(base);
+        r.layout = g.word(layout, "half", "interleaved");
+        r.order = g.word(order, "blocks", "turns");
+        if (!g.ok) return;
+        if (sections == Py_None) {
+            r.n_axes = 1;
+            r.sections[0] = (int32_t)(g.c->d / 2);
+            return;
+        }
+        const bool list = PyList_CheckExact(sections);
+        g.need(list || PyTuple_CheckExact(sections));
+        if (!g.ok) return;
+        const Py_ssize_t n = list ? PyList_GET_SIZE(sections) : PyTuple_GET_SIZE(sections);
+        g.need(n >= 1 && n <= 4);
+        for (Py_ssize_t i = 0; g.ok && i < n; ++i) r.sections[i] = g.i32(list ? PyList_GET_ITEM(sections, i) : PyTuple_GET_ITEM(sections, i));
+        r.n_axes = (int32_t)n;
+    }
+};
+
+// int32 [n_axes, n_tokens], or [n_tokens] for one axis; the elements between axes.
+const Tensor* positions_of(Args& g, PyObject* o, int64_t n_tokens, int64_t n_axes, int64_t* stride) {
+    const Tensor* t = g.tensor(o);
+    if (!t) return nullptr;
+    const bool flat = t->dim() == 1 && n_axes == 1;
+    g.need(here(t) && t->scalar_type() == at::kInt && (flat || (t->dim() == 2 && t->size(0) == n_axes)));
+    g.need(g.ok && t->size(-1) == n_tokens && t->stride(-1) == 1);
+    if (!g.ok) return nullptr;
+    *stride = n_axes > 1 ? t->stride(0) : n_tokens;
+    return t;
+}
+
+// k_pages, v_pages, token_start, kv_len, page_table: five arguments in a row
+struct Batch {
+    rekv_paged b;
+    Batch(Args& g, PyObject* kp, PyObject* vp, PyObject* start, PyObject* len, PyObject* table, int64_t n_tokens) : b{} {
+        const Tensor *k = g.keys(kp, 4), *v = g.keys(vp, 4), *t[3] = {g.tensor(start), g.tensor(len), g.tensor(table)};
+        if (!g.ok) return;
+        g.need(here(k) && here(v) && v->sizes() == k->sizes() && Args::fits(k->size(0)) && Args::fits(k->size(1)) && Args::fits(n_tokens));
+        for (int i = 0; i < 3; ++i)
+            g.need(g.ok && here(t[i]) && t[i]->scalar_type() == at::kInt && t[i]->dim() == (i == 2 ? 2 : 1) && t[i]->stride(-1) == 1);
+        if (!g.ok) return;
+        const int64_t n = t[1]->size(0);
+        g.need(Args::fits(n) && t[0]->size(0) == n + 1 && t[2]->size(0) == n && Args::fits(t[2]->size(1)));
+        if (!g.ok) return;
+        b.k_pages = k->data_ptr();
+        b.v_pages = v->data_ptr();
+        b.token_start = static_cast<const int32_t*>(t[0]->data_ptr());
+        b.kv_len = static_cast<const int32_t*>(t[1]->data_ptr());
+        b.page_table = static_cast<const int32_t*>(t[2]->data_ptr());
+        b.table_stride = n > 1 ? t[2]->stride(0) : t[2]->size(1);
+        b.max_pages = (int32_t)t[2]->size(1);
+        b.n_pages = (int32_t)k->size(0);
+        b.page_size = (int32_t)k->size(1);
+        b.n_seqs = (int32_t)n;
+        b.n_tokens = (int32_t)n_tokens;
+    }
+};
+
+METHOD(rotate, 8) {              // x, positions, sections, base, layout, order, inverse, out
+    Args g(self);
+    int64_t xs = 0, ps = 0, os = 0;
+    const Tensor* x = token_rows(g, a[0], -1, &xs);
+    Rotation rot(g, a[2], a[3], a[4], a[5]);
+    rot.r.inverse = g.flag(a[6]);
+    if (!g.ok) return nullptr;
+    const Tensor* pos = positions_of(g, a[1], x->size(0), rot.r.n_axes, &ps);
+    if (!g.ok) return nullptr;
+    Out out(a[7]);
+    if (!out.given) out.made = at::empty(x->sizes(), x->options());
+    const Tensor* o = out.given ? token_rows(g, a[7], x->size(1), &os) : &out.made;
+    g.need(g.ok && o->sizes() == x->sizes());
+    if (!g.ok) return nullptr;
+    if (!out.given) os = x->size(1) * x->size(2);
+    void* s = stream();
+    const rekv_status st = outside(rekv_rotate, g.c->h, (const rekv_rotary*)&rot.r, ptr(*x), xs, (int32_t)x->size(0), (int32_t)x->size(1),
+                                   static_cast<const int32_t*>(ptr(*pos)), ps, ptr(*o), os, s);
+    return st ? raise_status(g.c, st) : out.take();
+}
+
+METHOD(append_kv, 15) {          // k, v, k_pages, v_pages, token_start, kv_len, page_table, q, positions, sections, base, layout, order, rotate, q_out
+    Args g(self);
+    int64_t ks = 0, vs = 0, qs = 0, ps = 0, os = 0;
+    const Tensor *k = token_rows(g, a[0], g.c->hkv, &ks), *v = token_rows(g, a[1], g.c->hkv, &vs);
+    const bool turn = g.flag(a[13]), with_q = a[7] != Py_None;
+    Rotation rot(g, a[9], a[10], a[11], a[12]);
+    if (!g.ok) return nullptr;
+    const int64_t n = k->size(0);
+    Batch b(g, a[2], a[3], a[4], a[5], a[6], n);
+    g.need(g.ok && v->size(0) == n);
+    const Tensor *pos = nullptr, *q = nullptr, *qo = nullptr;
+    if (turn && a[8] != Py_None) pos = positions_of(g, a[8], n, rot.r.n_axes, &ps);
+    g.need(turn || a[8] == Py_None);
+    Out out(a[14]);
+    if (with_q) {
+        q = token_rows(g, a[7], g.c->hq, &qs);
+        g.need(g.ok && q->size(0) == n);
+        if (g.ok && !out.given) out.made = at::empty(q->sizes(), q->options());
+        if (g.ok && out.given) g.need((qo = token_rows(g, a[14], g.c->hq, &os)) && qo->is_contiguous() && qo->size(0) == n);
+    } else {
+        g.need(!out.given);
+    }
+    if (!g.ok) return nullptr;
+    void* s = stream();
+    const rekv_status st = outside(rekv_append_kv, g.c->h, (const rekv_paged*)&b.b, turn ? (const rekv_rotary*)&rot.r : nullptr, ptr(*k), ks, ptr(*v), vs,
+                                   with_q ? ptr(*q) : nullptr, qs, with_q ? ptr(out.get()) : nullptr,
+                                   pos ? static_cast<const int32_t*>(ptr(*pos)) : nullptr, ps, s);
+    if (st) return raise_status(g.c, st);
+    if (!with_q) return Py_NewRef(Py_False);     // done, without a result
+    return out.take();
+}
+
+// The attention of a batch over its pages; prefix == NULL: none.
+PyObject* run_paged(Args& g, const Batch& b, const Tensor* q, const Tensor* prefix, int32_t n_prefix, PyObject* max_kv, int32_t window,
+                          int32_t sinks, PyObject* out_) {
+    const int64_t most = (int64_t)b.b.max_pages * b.b.page_size;
+    const int32_t kv = max_kv == Py_None ? (int32_t)(most < (1 << 30) ? most : (1 << 30)) : g.i32(max_kv);
+    Out out(out_);
+    if (g.ok && !out.given) out.made = at::empty_like(*q);
+    else g.need(g.ok && g.queries(out_, 3) && here(&out.get()) && out.get().sizes() == q->sizes());
+    if (!g.ok) return nullptr;
+    int64_t bytes = 0;
+    rekv_status st = rekv_attention_paged_workspace(g.c->h, b.b.n_tokens, b.b.n_seqs, kv, window, sinks, n_prefix, &bytes);
+    if (st) return raise_status(g.c, st);
+    Tensor ws;
+    if (bytes) ws = at::empty({bytes}, on(*q, at::kByte));
+    void *s = stream(), *w = bytes ? ws.data_ptr() : nullptr;
+    if (prefix)
+        st = outside(rekv_attention_shared_prefix, g.c->h, (const rekv_paged*)&b.b, ptr(*q), static_cast<const int32_t*>(ptr(*prefix)), n_prefix, kv,
+                     ptr(out.get()), w, bytes, s);
+    else
+        st = outside(rekv_attention_paged, g.c->h, (const rekv_paged*)&b.b, ptr(*q), kv, window, sinks, ptr(out.get()), w, bytes, s);
+    return st ? raise_status(g.c, st) : out.take();
+}
+
+METHOD(attention_paged, 10) {    // q, k_pages, v_pages, token_start, kv_len, page_table, max_kv, window, sinks, out
+    Args g(self);
+    const Tensor* q = g.queries(a[0], 3);
+    const int32_t window = a[7] == Py_None ? -1 : g.i32(a[7]), sinks = g.i32(a[8]);
+    g.need(g.ok && here(q) && (a[7] == Py_None || window >= 0));
+    if (!g.ok) return nullptr;
+    Batch b(g, a[1], a[2], a[3], a[4], a[5], q->size(0));
+    if (!g.ok) return nullptr;
+    return run_paged(g, b, q, nullptr, 0, a[6], window, sinks, a[9]);
+}
+
+METHOD(attention_shared_prefix, 10) {   // q, k_pages, v_pages, prefix_pages, n_prefix, token_start, kv_len, page_table, max_kv, out
+    Args g(self);
+    const Tensor *q = g.queries(a[0], 3), *prefix = g.device(a[3], 1, at::kInt);
+    const int32_t n_prefix = g.i32(a[4]);
+    g.need(g.ok && here(q) && here(prefix));
+    if (!g.ok) return nullptr;
+    Batch b(g, a[1], a[2], a[5], a[6], a[7], q->size(0));
+    g.need(g.ok && n_prefix >= 1 && prefix->size(0) * b.b.page_size >= n_prefix);
+    if (!g.ok) return nullptr;
+    return run_paged(g, b, q, prefix, n_prefix, a[8], -1, 0, a[9]);
+}
+
 // The context is gone: every later call is the Python method's.
 PyObject* close_context(PyObject* self, PyObject*) {
     reinterpret_cast<Context*>(self)->h = nullptr;
@@ -492,7 +669,8 @@ int init_context(PyObject* self, PyObject* args, PyObject*) {
 PyMethodDef methods[] = {
     ENTRY(encode_chunk), ENTRY(frame_keys), ENTRY(retrieve_topk), ENTRY(retrieve_external), ENTRY(block_keys), ENTRY(expand_blocks),
     ENTRY(gather_kv), ENTRY(gather_kv_layers), ENTRY(gather_kv_rope), ENTRY(attention_indexed), ENTRY(attention_indexed_rope),
-    ENTRY(qa_attention), ENTRY(decode_attention), {"close", close_context, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+    ENTRY(qa_attention), ENTRY(decode_attention), ENTRY(rotate), ENTRY(append_kv), ENTRY(attention_paged), ENTRY(attention_shared_prefix),
+    {"close", close_context, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 
 PyTypeObject context_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 

@@ -147,6 +147,71 @@ hipError_t gather_rope_launch(const void* src_k, const void* src_v, bool src_on_
                               const int32_t* idx, int n_questions, int k_slots, int n_f, int n_kv_heads, int d,
                               int dtype, void* dst_k, void* dst_v, const RopeArgs& ra, hipStream_t stream);
 
+// Division by a launch constant of numbers below 2^31: with 2^(l-1) < d <= 2^l and m = ceil(2^(31+l) / d), which has 32
+// bits, n * m >> (31 + l) is exact, since m * d exceeds 2^(31+l) by less than 2^l and n is below 2^31.
+struct Div31 {
+    uint32_t d, m, shift;
+};
+inline Div31 div31(uint32_t d) {
+    uint32_t l = 0;
+    while ((1ull << l) < d) ++l;
+    return Div31{d, (uint32_t)(((1ull << (31 + l)) + d - 1) / d), l ? l - 1 : 0};
+}
+__device__ inline uint32_t quot(uint32_t n, const Div31& f) { return f.d > 1 ? __umulhi(n, f.m) >> f.shift : n; }
+
+// A batch over a paged cache (rekv_paged), and the attention of its new tokens.
+struct PagedBatch {
+    void *k_pages, *v_pages;            // [n_pages, page_size, Hkv, D]
+    const int32_t *token_start, *kv_len, *page_table;
+    int64_t table_stride;
+    int32_t max_pages, n_pages, n_seqs, n_tokens;
+    int32_t capacity;                   // max_pages * page_size
+    Div31 by_page;                      // d: page_size
+};
+struct PagedProblem {
+    PagedBatch b;
+    const void* q;
+    void* out;
+    const int32_t* prefix_pages;
+    int32_t n_prefix;                   // 0: none
+    int32_t window, sinks;              // window < 0: none
+    int32_t n_q_heads, n_kv_heads, head_dim;
+    float scale;
+};
+// How a launch is split: row blocks of `rows` stacked rows for the sequences' own tokens and, where the prefix is computed
+// for the whole batch at once (prefix_blocks > 0), for the prefix; splits of the keys of either; a partial result
+// per row and split where there is more than one in all.
+struct PagedPlan {
+    int32_t rows, blocks, splits, prefix_blocks, prefix_splits;
+    int32_t min_tiles;                  // a split has at least so many 32-key tiles
+    int64_t workspace_bytes;
+    int32_t slots() const { return splits + (prefix_blocks > 0 ? prefix_splits : 0); }
+};
+PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim, int64_t n_tokens, int64_t n_seqs, int64_t max_kv,
+                          int64_t window, int64_t sinks, int64_t n_prefix);
+hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int dtype, void* workspace, hipStream_t stream);
+
+// Rotary positions of one call: turns per position and axis of every pair.
+constexpr int MAX_PAIRS = 128, MAX_AXES = 4;
+struct Rotary {
+    double turns[MAX_PAIRS];            // base^(-2i / D) / (2 pi), negative for the inverse
+    uint8_t axis[MAX_PAIRS];
+    int32_t n_axes, interleaved;        // n_axes 0: no rotation
+};
+struct RotateArgs {
+    Rotary r;
+    const int32_t* positions;           // NULL: index in the sequence (append only)
+    int64_t positions_stride;
+    int32_t n_tokens, head_dim, n_q_heads, n_kv_heads;
+    const void* q;                      // rotate: x
+    void* q_out;
+    int64_t q_stride, q_out_stride;
+    const void *k, *v;                  // NULL: rotate only
+    int64_t k_stride, v_stride;
+    PagedBatch b;
+};
+hipError_t rotate_launch(const RotateArgs& a, int dtype, hipStream_t stream);
+
 // Measurement probes (probe.hip).
 hipError_t launch_probe_copy(void* dst, const void* src, int64_t n_bytes, hipStream_t stream);
 hipError_t launch_probe_mfma(float* sink, int32_t n_workgroups, int32_t n_iters, hipStream_t stream);

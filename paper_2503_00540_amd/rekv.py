@@ -30,12 +30,24 @@ _DTYPES = {"f32": (REKV_F32, torch.float32), "bf16": (REKV_BF16, torch.bfloat16)
 SYMBOLS = ("rekv_create", "rekv_destroy", "rekv_last_error", "rekv_encode_chunk",
            "rekv_frame_keys", "rekv_retrieve_topk", "rekv_gather_kv", "rekv_qa_attention",
            "rekv_decode_attention", "rekv_decode_attention_noalloc", "rekv_block_keys", "rekv_expand_blocks", "rekv_retrieve_external", "rekv_attention_indexed", "rekv_gather_kv_rope", "rekv_gather_kv_layers", "rekv_attention_indexed_rope",
-           "rekv_offload_kv", "rekv_offload_wait", "rekv_offload_join", "rekv_probe_copy", "rekv_probe_mfma")
+           "rekv_offload_kv", "rekv_offload_wait", "rekv_offload_join", "rekv_rotate", "rekv_append_kv", "rekv_attention_paged",
+           "rekv_attention_shared_prefix", "rekv_attention_paged_workspace", "rekv_probe_copy", "rekv_probe_mfma")
 
 
 class RekvShape(ctypes.Structure):
     _fields_ = [("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32),
                 ("tokens_per_frame", c_int32), ("dtype", c_int32), ("softmax_scale", c_float)]
+
+
+class RekvPaged(ctypes.Structure):
+    _fields_ = [("k_pages", c_void_p), ("v_pages", c_void_p), ("token_start", c_void_p), ("kv_len", c_void_p), ("page_table", c_void_p),
+                ("table_stride", c_int64), ("max_pages", c_int32), ("n_pages", c_int32), ("page_size", c_int32), ("n_seqs", c_int32),
+                ("n_tokens", c_int32)]
+
+
+class RekvRotary(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("layout", c_int32), ("order", c_int32), ("inverse", c_int32), ("n_axes", c_int32),
+                ("sections", c_int32 * 4)]
 
 
 class RekvError(RuntimeError):
@@ -94,6 +106,13 @@ def lib() -> ctypes.CDLL:
                                   c_void_p]
     L.rekv_offload_wait.argtypes = [c_void_p]
     L.rekv_offload_join.argtypes = [c_void_p, c_void_p]
+    L.rekv_rotate.argtypes = [c_void_p, POINTER(RekvRotary), c_void_p, c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64, c_void_p]
+    L.rekv_append_kv.argtypes = [c_void_p, POINTER(RekvPaged), POINTER(RekvRotary), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64,
+                                 c_void_p, c_void_p, c_int64, c_void_p]
+    L.rekv_attention_paged.argtypes = [c_void_p, POINTER(RekvPaged), c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_int64, c_void_p]
+    L.rekv_attention_shared_prefix.argtypes = [c_void_p, POINTER(RekvPaged), c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int64,
+                                               c_void_p]
+    L.rekv_attention_paged_workspace.argtypes = [c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, POINTER(c_int64)]
     L.rekv_probe_copy.argtypes = [c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
     L.rekv_probe_mfma.argtypes = [c_void_p, c_void_p, c_int32, c_int32, POINTER(ctypes.c_double), c_void_p]
     for name in SYMBOLS[3:]:
@@ -514,6 +533,158 @@ class Rekv:
             self._n_sel(n_sel, nq), self._dev(k_text, last=kh, name="k_text"), self._dev(v_text, last=kh, name="v_text"),
             k_text.shape[1], n_text_tokens, nq, n_new, self._dev(out, last=qh, name="out"), _stream()))
         return out
+
+    # -- many streams and users on one paged cache -----------------------------------------
+    def _here(self, **tensors):
+        """All on the current device, which is where the call's launches go."""
+        device = torch.cuda.current_device() if torch.cuda.is_available() else None
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a CUDA tensor")
+            if t.device.index != device:
+                raise ValueError(f"{name} lives on {t.device}, the current device is cuda:{device}")
+
+    def _tokens(self, t, heads, name) -> int:
+        """[tokens, heads, D] whose head vectors lie side by side; returns the elements between tokens."""
+        if t.dim() != 3 or t.dtype is not self.torch_dtype or t.shape[2] != self.head_dim or (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {self.head_dim}] of {self.torch_dtype}, got {tuple(t.shape)} of {t.dtype}")
+        if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim):
+            raise ValueError(f"{name}: the head vectors of a token must lie side by side")
+        return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+    def _positions(self, positions, n_tokens, n_axes):
+        """[n_axes, n_tokens] (or [n_tokens] for one axis) int32; returns the elements between axes."""
+        if positions.dim() == 1 and n_axes == 1:
+            positions = positions[None]
+        if positions.dim() != 2 or positions.dtype != torch.int32 or tuple(positions.shape) != (n_axes, n_tokens) or positions.stride(1) != 1:
+            raise ValueError(f"positions must be int32 [{n_axes}, {n_tokens}] with a token's neighbours side by side, got {tuple(positions.shape)} "
+                             f"of {positions.dtype}")
+        return positions.stride(0) if n_axes > 1 else n_tokens
+
+    def _rotary(self, sections, base, layout, order, inverse=False):
+        sections = [self.head_dim // 2] if sections is None else list(sections)
+        if not 1 <= len(sections) <= 4:
+            raise ValueError("sections must name 1 to 4 axes")
+        return RekvRotary(base, {"half": 0, "interleaved": 1}[layout], {"blocks": 0, "turns": 1}[order], int(inverse), len(sections),
+                          (c_int32 * 4)(*sections))
+
+    def _paged(self, k_pages, v_pages, token_start, kv_len, page_table, n_tokens):
+        kh = (self.n_kv_heads, self.head_dim)
+        self._here(k_pages=k_pages, v_pages=v_pages, token_start=token_start, kv_len=kv_len, page_table=page_table)
+        if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+            raise ValueError("k_pages / v_pages must both be [n_pages, page_size, Hkv, D]")
+        for t, dims, name in ((token_start, 1, "token_start"), (kv_len, 1, "kv_len"), (page_table, 2, "page_table")):
+            if t.dim() != dims or t.dtype != torch.int32 or t.stride(-1) != 1:
+                raise ValueError(f"{name} must be int32 with {dims} dimension(s), neighbours side by side")
+        n_seqs = kv_len.shape[0]
+        if token_start.shape[0] != n_seqs + 1 or page_table.shape[0] != n_seqs:
+            raise ValueError("token_start must be [n_seqs + 1], kv_len [n_seqs], page_table [n_seqs, pages]")
+        return RekvPaged(self._dev(k_pages, last=kh, name="k_pages"), self._dev(v_pages, last=kh, name="v_pages"), token_start.data_ptr(),
+                         kv_len.data_ptr(), page_table.data_ptr(), page_table.stride(0) if n_seqs > 1 else page_table.shape[1],
+                         page_table.shape[1], k_pages.shape[0], k_pages.shape[1], n_seqs, n_tokens)
+
+    def rotate(self, x, positions, sections=None, base: float = 10000.0, layout: str = "half", order: str = "blocks",
+               inverse: bool = False, out=None):
+        """rekv_rotate: x [n_tokens, n_heads, D] (tokens may lie apart, as in a fused projection), positions int32 [n_axes, n_tokens] or
+        [n_tokens]; sections: rotary pairs of each axis (None: one axis).  out may be x."""
+        done = self._fast.rotate(x, positions, sections, base, layout, order, inverse, out)
+        if done is not None:
+            return done
+        self._here(x=x, positions=positions, out=out)
+        x_stride = self._tokens(x, None, "x")
+        rotary = self._rotary(sections, base, layout, order, inverse)
+        p_stride = self._positions(positions, x.shape[0], rotary.n_axes)
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+        out_stride = self._tokens(out, x.shape[1], "out")
+        if out.shape != x.shape:
+            raise ValueError("out must have the shape of x")
+        self._check(self._lib.rekv_rotate(self._h, byref(rotary), x.data_ptr(), x_stride, x.shape[0], x.shape[1], positions.data_ptr(),
+                                          p_stride, out.data_ptr(), out_stride, _stream()))
+        return out
+
+    def append_kv(self, k, v, k_pages, v_pages, token_start, kv_len, page_table, q=None, positions=None, sections=None,
+                  base: float = 10000.0, layout: str = "half", order: str = "blocks", rotate: bool = True, q_out=None):
+        """rekv_append_kv: k, v [n_tokens, Hkv, D] (and q [n_tokens, Hq, D]; tokens may lie apart) of a ragged batch into the pages
+        [n_pages, page_size, Hkv, D]; kv_len counts the new tokens.  positions None: a token's index in its sequence.  Returns the
+        rotated queries [n_tokens, Hq, D], None without q."""
+        done = self._fast.append_kv(k, v, k_pages, v_pages, token_start, kv_len, page_table, q, positions, sections, base, layout, order, rotate,
+                                    q_out)
+        if done is not None:
+            return None if done is False else done
+        self._here(k=k, v=v, q=q, positions=positions, q_out=q_out)
+        n = k.shape[0]
+        cache = self._paged(k_pages, v_pages, token_start, kv_len, page_table, n)
+        k_stride, v_stride = self._tokens(k, self.n_kv_heads, "k"), self._tokens(v, self.n_kv_heads, "v")
+        q_stride = 0
+        if q is None and q_out is not None:
+            raise ValueError("q_out without q")
+        if q is not None:
+            q_stride = self._tokens(q, self.n_q_heads, "q")
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+            self._dev(q_out, last=(self.n_q_heads, self.head_dim), name="q_out")
+            if q.shape[0] != n or q_out.shape != q.shape:
+                raise ValueError("q and q_out must hold as many tokens as k")
+        if v.shape[0] != n:
+            raise ValueError("k and v must hold as many tokens")
+        rotary = self._rotary(sections, base, layout, order) if rotate else None
+        p_stride = 0 if positions is None or rotary is None else self._positions(positions, n, rotary.n_axes)
+        self._check(self._lib.rekv_append_kv(
+            self._h, byref(cache), byref(rotary) if rotate else None, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
+            q.data_ptr() if q is not None else None, q_stride, q_out.data_ptr() if q is not None else None,
+            positions.data_ptr() if p_stride else None, p_stride, _stream()))
+        return q_out
+
+    def _attention_paged(self, q, cache, n_prefix, prefix_pages, max_kv, window, sinks, out):
+        qh = (self.n_q_heads, self.head_dim)
+        if q.dim() != 3:
+            raise ValueError("q must be [n_tokens, Hq, D]")
+        max_kv = cache.max_pages * cache.page_size if max_kv is None else max_kv
+        out = torch.empty_like(q) if out is None else out
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+        pq, po = self._dev(q, last=qh, name="q"), self._dev(out, last=qh, name="out")
+        need = c_int64(0)
+        self._check(self._lib.rekv_attention_paged_workspace(self._h, cache.n_tokens, cache.n_seqs, max_kv, window, sinks, n_prefix, byref(need)))
+        # the caching allocator's blocks suit: ordered on the stream, and a graph's own under capture
+        ws = torch.empty((need.value,), dtype=torch.uint8, device=q.device) if need.value else None
+        pw = ws.data_ptr() if need.value else None
+        if n_prefix:
+            self._check(self._lib.rekv_attention_shared_prefix(self._h, byref(cache), pq, prefix_pages.data_ptr(), n_prefix, max_kv, po, pw,
+                                                               need.value, _stream()))
+        else:
+            self._check(self._lib.rekv_attention_paged(self._h, byref(cache), pq, max_kv, window, sinks, po, pw, need.value, _stream()))
+        return out
+
+    def attention_paged(self, q, k_pages, v_pages, token_start, kv_len, page_table, max_kv: int | None = None,
+                        window: int | None = None, sinks: int = 0, out=None):
+        """rekv_attention_paged: q [n_tokens, Hq, D] of a ragged batch over the pages [n_pages, page_size, Hkv, D].  window None: all
+        keys; otherwise the last `window` of them, the token itself among them, and the first `sinks`.  max_kv: about the
+        largest kv_len (None: what the table holds), for the split of the work only."""
+        done = self._fast.attention_paged(q, k_pages, v_pages, token_start, kv_len, page_table, max_kv, window, sinks, out)
+        if done is not None:
+            return done
+        self._here(q=q, out=out)
+        if window is not None and window < 0:
+            raise ValueError(f"window={window} must not be negative (None: no window)")
+        cache = self._paged(k_pages, v_pages, token_start, kv_len, page_table, q.shape[0])
+        return self._attention_paged(q, cache, 0, None, max_kv, -1 if window is None else window, sinks, out)
+
+    def attention_shared_prefix(self, q, k_pages, v_pages, prefix_pages, n_prefix: int, token_start, kv_len, page_table,
+                                max_kv: int | None = None, out=None):
+        """rekv_attention_shared_prefix: as attention_paged without a window, where every token also sees the n_prefix tokens in
+        prefix_pages (int32), computed once for the batch; kv_len and page_table count the own tokens only."""
+        done = self._fast.attention_shared_prefix(q, k_pages, v_pages, prefix_pages, n_prefix, token_start, kv_len, page_table, max_kv, out)
+        if done is not None:
+            return done
+        self._here(q=q, prefix_pages=prefix_pages, out=out)
+        cache = self._paged(k_pages, v_pages, token_start, kv_len, page_table, q.shape[0])
+        if prefix_pages.dim() != 1 or prefix_pages.dtype != torch.int32 or not prefix_pages.is_contiguous():
+            raise ValueError("prefix_pages must be contiguous int32 with one dimension")
+        if n_prefix < 1 or prefix_pages.shape[0] * cache.page_size < n_prefix:
+            raise ValueError(f"prefix_pages hold {prefix_pages.shape[0] * cache.page_size} tokens, n_prefix={n_prefix}")
+        return self._attention_paged(q, cache, n_prefix, prefix_pages, max_kv, -1, 0, out)
 
     def offload_kv(self, dev_k, dev_v, host_k, host_v, first_frame: int, n_frames: int):
         kh = (self.n_kv_heads, self.head_dim)
