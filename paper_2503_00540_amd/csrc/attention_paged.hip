@@ -52,25 +52,8 @@ struct Entries {
 struct Place {
     int64_t a, b;
     int rows_a;
+    bool whole;             // all rows see the tile whole
 };
-
-// Where a key's probability is 0 because its row does not see it, an infinity or NaN among the values would still make
-// NaN of the product.  Tiles that not every row sees whole leave such values out ...
-__device__ inline uint64_t drop_nonfinite(bf16x8& v) {
-    u32x4 w = __builtin_bit_cast(u32x4, v);
-    uint32_t any = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) any |= (w[i] & 0x7f807f80u) + 0x00800080u;      // bit 15 of a half: its exponent is all ones
-    const uint64_t lanes = __builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0);
-    if (lanes == 0) return 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
-        if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0x0000ffffu;
-    }
-    v = __builtin_bit_cast(bf16x8, w);
-    return lanes;
-}
 
 // TWO_PAGES: 32 keys from a multiple of 32 on lie in two pages at most (pages of 32 tokens or more, or of 16); otherwise every
 // lane looks its rows' pages up.
@@ -81,6 +64,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
     constexpr int N_DMA = BN / RPI / WAVES;   // such loads per wave, tile and tensor
     constexpr uint32_t TILE_B = BN * D * 2;
     __shared__ __attribute__((aligned(1024))) bf16_t lds[2 * STAGES * BN * D];
+    __shared__ int sh_dropped;
 
     const PagedProblem& p = a.p;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -156,34 +140,34 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
     auto place = [&](int t, Entries e) {
         const int k0 = tiles.key0(t), within = k0 - (int)quot((uint32_t)k0, p.b.by_page) * page;
         const int pa = clamped(e.a, 0, p.b.n_pages - 1), pb = clamped(e.b, 0, p.b.n_pages - 1);
-        return Place{((int64_t)pa * page + within) * row_b, ((int64_t)pb * page + within - page) * row_b, page - within};
+        return Place{((int64_t)pa * page + within) * row_b, ((int64_t)pb * page + within - page) * row_b, page - within, tiles.whole(t, 1)};
     };
-    // A tile whose 32 rows are all fetched as they are.
-    auto dma_whole = [&](const char* base, const Place& at, uint32_t stage_b) {
-        if (at.rows_a >= BN) {
-#pragma unroll
-            for (int j = 0; j < N_DMA; ++j) dma16<false>(base + at.a, dma_off[j], dma_lds + stage_b + j * 1024u);
-        } else {
-            const uint64_t pa = reinterpret_cast<uint64_t>(base + at.a), pb = reinterpret_cast<uint64_t>(base + at.b);
-#pragma unroll
-            for (int j = 0; j < N_DMA; ++j)
-                dma16_at((dma_row + j * RPI < at.rows_a ? pa : pb) + dma_off[j], dma_lds + stage_b + j * 1024u);
-        }
+    // Row r of a tile, by the page it lies in: lanes of either page take a load of their own, from a uniform address (where a
+    // load has lanes of both, one more is in flight than step_barrier counts, which only makes it wait longer).
+    auto dma_row_of = [&](const char* base, const Place& at, int r, uint32_t off, uint32_t dst) {
+        if (r < at.rows_a) dma16<false>(base + at.a, off, dst);
+        else dma16<false>(base + at.b, off, dst);
     };
-    // Any tile: the rows that no row of the block sees repeat the nearest that one does.
-    auto dma_any = [&](const char* base, int t, const Place& at, uint32_t stage_b) {
-        int r0, r1;
-        tiles.rows(t, &r0, &r1);
+    // Tile t; the rows that no row of the block sees repeat the nearest that one does.
+    auto dma_tile = [&](const char* base, int t, const Place& at, uint32_t stage_b) {
         if (TWO_PAGES) {
-            const uint64_t pa = reinterpret_cast<uint64_t>(base + at.a), pb = reinterpret_cast<uint64_t>(base + at.b);
+            if (at.whole && at.rows_a >= BN) {
+#pragma unroll
+                for (int j = 0; j < N_DMA; ++j) dma16<false>(base + at.a, dma_off[j], dma_lds + stage_b + j * 1024u);
+                return;
+            }
+            int r0 = 0, r1 = BN - 1;
+            if (!at.whole) tiles.rows(t, &r0, &r1);
 #pragma unroll
             for (int j = 0; j < N_DMA; ++j) {
                 const int r = clamped(dma_row + j * RPI, r0, r1);
-                dma16_at((r < at.rows_a ? pa : pb) + ((uint32_t)r * row_b + dma_coff[j]), dma_lds + stage_b + j * 1024u);
+                dma_row_of(base, at, r, (uint32_t)r * row_b + dma_coff[j], dma_lds + stage_b + j * 1024u);
             }
         } else {
             const int32_t* table = table_of(t);
             const int k0 = tiles.key0(t);
+            int r0, r1;
+            tiles.rows(t, &r0, &r1);
             uint64_t from[N_DMA];
 #pragma unroll
             for (int j = 0; j < N_DMA; ++j) {
@@ -213,7 +197,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
         for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
     float m_ref = -INFINITY, l_part = 0.f;
     const float sc = p.scale * 1.4426950408889634f;
-    uint64_t dropped = 0;                    // some lane left values out
 
     auto qk = [&](const bf16x8 (&kf)[D / 16], f32x16& s) {
 #pragma unroll
@@ -230,23 +213,52 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
     Entries e_next;
     Place at_k, at_v;
 
-    // One step, as in attention_bf16.hip.  PLAIN: tiles t to t + 4 are seen whole by all rows.
-    auto step = [&](int t, f32x16& s_cur, f32x16& s_next, auto kn, auto kl, auto vc, auto vl, auto plain) {
+    // A tile that not every row sees whole: probabilities of 0 keep a value out only if it is finite, so its infinities and NaNs
+    // become 0 in LDS (every wavefront sees to that for itself, before it reads the tile) and are added after the loop.
+    auto drop_nonfinite = [&](uint32_t stage_b) {
+        const uint32_t at = lds0 + STAGES * TILE_B + stage_b + lane * 16u;
+        uint32_t any = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < TILE_B; i += 1024) {
+            const u32x4 w = *reinterpret_cast<LDS_AS const u32x4*>(at + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) any |= (w[k] & 0x7f807f80u) + 0x00800080u;      // bit 15 of a half: its exponent is all ones
+        }
+        if (__builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0) == 0) return;
+        sh_dropped = 1;
+#pragma unroll 1
+        for (uint32_t i = 0; i < TILE_B; i += 1024) {
+            u32x4 w = *reinterpret_cast<LDS_AS const u32x4*>(at + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
+                if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0x0000ffffu;
+            }
+            *reinterpret_cast<LDS_AS u32x4*>(at + i) = w;
+        }
+    };
+
+    // One step, as in attention_bf16.hip.
+    auto step = [&](int t, f32x16& s_cur, f32x16& s_next, auto kn, auto kl, auto vc, auto vl) __attribute__((always_inline)) {
         constexpr uint32_t KN = decltype(kn)::value * TILE_B, KL = decltype(kl)::value * TILE_B;
         constexpr uint32_t VC = decltype(vc)::value * TILE_B, VL = decltype(vl)::value * TILE_B;
-        constexpr bool PLAIN = decltype(plain)::value;
         if (TWO_PAGES) {
             at_v = at_k;
             at_k = place(in_list(t + 4), e_next);
         }
-        if (PLAIN && TWO_PAGES) {
-            dma_whole(k_base, at_k, KL);
-            dma_whole(v_base, at_v, STAGES * TILE_B + VL);
-        } else {
-            dma_any(k_base, in_list(t + 4), at_k, KL);
-            dma_any(v_base, in_list(t + 3), at_v, STAGES * TILE_B + VL);
-        }
+        dma_tile(k_base, in_list(t + 4), at_k, KL);
+        dma_tile(v_base, in_list(t + 3), at_v, STAGES * TILE_B + VL);
         if (TWO_PAGES) e_next = entries(in_list(t + 5));
+        if (!tiles.whole(t, 1)) {
+            const int k0 = tiles.key0(t);
+            const bool pre = tiles.in_prefix(t);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int key = k0 + (j >> 2) * 8 + hh * 4 + (j & 3);
+                s_cur[j] = (pre ? key < tiles.n_prefix : sees(p, pos, row_hi, key)) ? s_cur[j] : -INFINITY;
+            }
+            drop_nonfinite(VC);
+        }
         bf16x8 kf[D / 16];
         load_k(KN, kf);
         bf16x8 vf[2][D / 32];
@@ -263,16 +275,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
         };
         load_v(0);
         __builtin_amdgcn_sched_barrier(0);
-        const bool masked = !PLAIN && !tiles.whole(t, 1);
-        if (masked) {
-            const int k0 = tiles.key0(t);
-            const bool pre = tiles.in_prefix(t);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int key = k0 + (j >> 2) * 8 + hh * 4 + (j & 3);
-                s_cur[j] = (pre ? key < tiles.n_prefix : sees(p, pos, row_hi, key)) ? s_cur[j] : -INFINITY;
-            }
-        }
         float mx = s_cur[0];
 #pragma unroll
         for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s_cur[j]);
@@ -294,10 +296,6 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
         load_v(1);
 #pragma unroll
         for (int g16 = 0; g16 < 2; ++g16) {
-            if (masked) {
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db) dropped |= drop_nonfinite(vf[g16][db]);
-            }
             float e[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -326,14 +324,15 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
     };
 
     if (t_begin < t_end) {
+        if (tid == 0) sh_dropped = 0;        // before the first barrier
         f32x16 s_a, s_b;
         constexpr uint32_t VB = STAGES * TILE_B;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {        // K of four tiles, V of three
             const int t = in_list(t_begin + i);
             if (TWO_PAGES) at_k = place(t, entries(t));
-            dma_any(k_base, t, at_k, i * TILE_B);
-            if (i < 3) dma_any(v_base, t, at_k, VB + i * TILE_B);
+            dma_tile(k_base, t, at_k, i * TILE_B);
+            if (i < 3) dma_tile(v_base, t, at_k, VB + i * TILE_B);
         }
         if (TWO_PAGES) e_next = entries(in_list(t_begin + 4));
         step_barrier<0>();
@@ -352,37 +351,27 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
                     at_v = at_k;
                     at_k = place(in_list(t + 4), e_next);
                 }
-                dma_any(k_base, in_list(t + 4), at_k, i4 * TILE_B);
-                dma_any(v_base, in_list(t + 3), at_v, VB + ((i4 + 3u) & 3u) * TILE_B);
+                dma_tile(k_base, in_list(t + 4), at_k, i4 * TILE_B);
+                dma_tile(v_base, in_list(t + 3), at_v, VB + ((i4 + 3u) & 3u) * TILE_B);
                 if (TWO_PAGES) e_next = entries(in_list(t + 5));
                 step_barrier<2 * DMA_PER_STEP>();
             }
         }
-        const std::false_type general;
-        const std::true_type plain;
         while (t < t_end) {
-            if (TWO_PAGES && t + 8 <= t_end && tiles.whole(t, 8)) {
-                step(t, s_a, s_b, IC<1>{}, IC<0>{}, IC<0>{}, IC<3>{}, plain);
-                step(t + 1, s_b, s_a, IC<2>{}, IC<1>{}, IC<1>{}, IC<0>{}, plain);
-                step(t + 2, s_a, s_b, IC<3>{}, IC<2>{}, IC<2>{}, IC<1>{}, plain);
-                step(t + 3, s_b, s_a, IC<0>{}, IC<3>{}, IC<3>{}, IC<2>{}, plain);
-                t += 4;
-                continue;
-            }
-            step(t, s_a, s_b, IC<1>{}, IC<0>{}, IC<0>{}, IC<3>{}, general);
+            step(t, s_a, s_b, IC<1>{}, IC<0>{}, IC<0>{}, IC<3>{});
             if (++t == t_end) break;
-            step(t, s_b, s_a, IC<2>{}, IC<1>{}, IC<1>{}, IC<0>{}, general);
+            step(t, s_b, s_a, IC<2>{}, IC<1>{}, IC<1>{}, IC<0>{});
             if (++t == t_end) break;
-            step(t, s_a, s_b, IC<3>{}, IC<2>{}, IC<2>{}, IC<1>{}, general);
+            step(t, s_a, s_b, IC<3>{}, IC<2>{}, IC<2>{}, IC<1>{});
             if (++t == t_end) break;
-            step(t, s_b, s_a, IC<0>{}, IC<3>{}, IC<3>{}, IC<2>{}, general);
+            step(t, s_b, s_a, IC<0>{}, IC<3>{}, IC<3>{}, IC<2>{});
             ++t;
         }
         wait_vmem();               // no load may still be writing LDS when the workgroup retires
     }
 
-    // ... and add them to the rows that do see them, from memory, key by key.
-    if (dropped != 0 && row_ok) {
+    // The values left out, for the rows that do see them: from memory, key by key.  (A step's last barrier is behind every write.)
+    if (t_begin < t_end && sh_dropped != 0 && row_ok) {
         const float mr = (m_ref == -INFINITY) ? 0.f : m_ref;
         const bf16_t* qr = static_cast<const bf16_t*>(p.q) + q_row * D;
 #pragma unroll 1
