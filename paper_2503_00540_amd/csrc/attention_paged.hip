@@ -18,10 +18,11 @@
 namespace rekv {
 namespace {
 
-constexpr int STAGES = 4;
 constexpr int WAVES = 4;
-constexpr int WM = 32;
-constexpr int BM = WAVES * WM;
+constexpr int THREADS = WAVES * 64;
+constexpr int WM = 32;                // rows of a wavefront
+constexpr int BM = WAVES * WM;        // rows of a block whose wavefronts share the tiles
+constexpr int STAGES = 4;             // of such a block, per tensor
 
 struct PagedArgs {
     PagedProblem p;
@@ -30,6 +31,342 @@ struct PagedArgs {
     float* part_ml;       // [slot][token * Hq + head][2]: maximum (of base-2 exponents), sum
 };
 
+// As dma16 (attention_mfma.h), from a 64-bit address per lane.
+__device__ inline void dma16_at(uint64_t addr, uint32_t lds_addr) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+                 ::"v"(addr), "s"(__builtin_amdgcn_readfirstlane(lds_addr)) : "memory", "m0");
+}
+
+// Where a tile lies.  Pages of 32 tokens or more, or of 16 (TWO_PAGES): the cache's row (page * page_size + row) that the tile's
+// row 0 is in its first page and would be in its next, and how many rows lie in the first (32: all).  Smaller pages: every
+// lane's row.  whole: all rows of the block see the tile whole.
+struct Place {
+    int a, b, rows_a;
+    bool whole;
+};
+// The places of 64 tiles from t0 on, one per lane.  Worked out at once, with one wait for the page table, they cost a step two or
+// three lane reads, where following the list step by step cost it about 80 scalar instructions.
+struct Places {
+    int t0, a, b, rows_whole;
+};
+
+// A block's tiles and their way into LDS, by LOADERS wavefronts together.
+template <int D, bool TWO_PAGES, int LOADERS, bool STREAM>
+struct Source {
+    static constexpr int CH = D / 8;                       // 16-byte chunks per key row
+    static constexpr int RPI = 64 / CH;                    // key rows one 1 KB wave-wide load covers
+    static constexpr int N_DMA = BN / RPI / LOADERS;       // such loads per wave, tile and tensor
+    static constexpr int N_OFF = N_DMA < 16 / RPI ? N_DMA : 16 / RPI;      // the swizzle repeats every 16 rows
+    static constexpr uint32_t TILE_B = BN * D * 2;         // bytes of a tile
+
+    const PagedProblem& p;
+    const Job& job;
+    const Tiles<BN>& tiles;
+    int t_end, lane, loader;
+    const char *k_base, *v_base;
+    uint32_t row_b;                                        // bytes of a token's keys
+    int first_row;                                         // of this lane
+    uint32_t off[N_OFF];                                   // byte offset in a whole tile of what load j fetches
+
+    __device__ Source(const PagedProblem& p_, const Job& job_, const Tiles<BN>& tiles_, int t_end_, int kvh, int lane_, int loader_)
+        : p(p_), job(job_), tiles(tiles_), t_end(t_end_), lane(lane_), loader(loader_) {
+        row_b = (uint32_t)p.n_kv_heads * D * 2u;
+        k_base = static_cast<const char*>(p.b.k_pages) + kvh * D * 2;
+        v_base = static_cast<const char*>(p.b.v_pages) + kvh * D * 2;
+        first_row = loader * N_DMA * RPI + lane / CH;
+#pragma unroll
+        for (int j = 0; j < N_OFF; ++j) off[j] = (uint32_t)(first_row + j * RPI) * row_b + chunk(first_row + j * RPI);
+    }
+    __device__ uint32_t chunk(int row) const { return (uint32_t)((lane % CH) ^ swz<D>(row)) * 16u; }
+    __device__ int in_list(int t) const { return t < t_end ? t : t_end - 1; }
+
+    __device__ __attribute__((always_inline)) void fill(Places& at, int t0) const {
+        at.t0 = t0;
+        if (!TWO_PAGES) return;
+        const int t = in_list(t0 + lane), page = (int)p.b.by_page.d, k0 = tiles.key0(t);
+        const bool pre = tiles.in_prefix(t);
+        const int32_t* table = pre ? p.prefix_pages : job.table;
+        const int last = pre ? (int)quot((uint32_t)(tiles.n_prefix - 1), p.b.by_page) : p.b.max_pages - 1;
+        const int slot = (int)quot((uint32_t)k0, p.b.by_page), within = k0 - slot * page;
+        const int a = clamped(table[slot], 0, p.b.n_pages - 1), b = clamped(table[slot < last ? slot + 1 : last], 0, p.b.n_pages - 1);
+        const int rows_a = page - within < BN ? page - within : BN;
+        at.a = a * page + within;
+        at.b = b * page + within - page;
+        at.rows_whole = rows_a * 2 + tiles.whole(t);
+    }
+    // Of tile t; the 64 tiles move on where it is behind them.
+    __device__ __attribute__((always_inline)) Place place(Places& from, int t) const {
+        Place at;
+        if (t - from.t0 >= 64) fill(from, t);
+        if (TWO_PAGES) {
+            const int i = t - from.t0, rw = __builtin_amdgcn_readlane(from.rows_whole, i);
+            at.a = __builtin_amdgcn_readlane(from.a, i);
+            at.b = __builtin_amdgcn_readlane(from.b, i);
+            at.rows_a = rw >> 1;
+            at.whole = rw & 1;
+        } else {
+            at.whole = tiles.whole(t);
+            int r0, r1;
+            tiles.rows(t, &r0, &r1);
+            const int k0 = tiles.key0(t), page = (int)p.b.by_page.d;
+            const int32_t* table = tiles.in_prefix(t) ? p.prefix_pages : job.table;
+            if (LOADERS > 1) {               // eight rows of this wavefront: lane i (of eight) gets the place of row i
+                const int base = loader * N_DMA * RPI;
+                static_assert(LOADERS == 1 || N_DMA * RPI == 8, "below");
+                at.a = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {      // through the scalar cache: waiting for it does not wait for tile loads
+                    const int key = k0 + clamped(base + i, r0, r1), slot = (int)quot((uint32_t)key, p.b.by_page);
+                    const int row = clamped(scalar_word(table, slot), 0, p.b.n_pages - 1) * page + (key - slot * page);
+                    at.a = (lane & 7) == i ? row : at.a;
+                }
+            } else {
+                const int key = k0 + clamped(lane & 31, r0, r1), slot = (int)quot((uint32_t)key, p.b.by_page);
+                at.a = clamped(table[slot], 0, p.b.n_pages - 1) * page + (key - slot * page);
+            }
+        }
+        return at;
+    }
+    // Row r of a tile in two pages: lanes of either take a load of their own, from a uniform address.  Where a load has lanes
+    // of both, one more is in flight than is counted below, which only makes a wait longer.
+    __device__ __attribute__((always_inline)) void fetch_row(const char* base, const Place& at, int r, uint32_t o, uint32_t dst) const {
+        if (r < at.rows_a) dma16<STREAM>(base + at.a * (int64_t)row_b, o, dst);
+        else dma16<STREAM>(base + at.b * (int64_t)row_b, o, dst);
+    }
+    // This wavefront's share of a tile.  Rows that no row of the block sees repeat the nearest that one does.
+    __device__ __attribute__((always_inline)) void fetch(const char* base, int t, const Place& at, uint32_t dst) const {
+        dst += (uint32_t)(loader * N_DMA) * 1024u;
+        if (!TWO_PAGES) {
+#pragma unroll
+            for (int j = 0; j < N_DMA; ++j) {
+                const int r = first_row + j * RPI, row = __shfl(at.a, LOADERS > 1 ? r & 7 : r);
+                dma16_at(reinterpret_cast<uint64_t>(base) + (uint64_t)(uint32_t)row * row_b + chunk(r), dst + j * 1024u);
+            }
+        } else if (at.whole && at.rows_a >= BN) {
+#pragma unroll
+            for (int j = 0; j < N_DMA; ++j)
+                dma16<STREAM>(base + (int64_t)(at.a + j / N_OFF * 16) * row_b, off[j % N_OFF], dst + j * 1024u);
+        } else {
+            int r0 = 0, r1 = BN - 1;
+            if (!at.whole) tiles.rows(t, &r0, &r1);
+            if (N_DMA <= 2) {
+#pragma unroll
+                for (int j = 0; j < N_DMA; ++j) {
+                    const int r = clamped(first_row + j * RPI, r0, r1);
+                    fetch_row(base, at, r, (uint32_t)r * row_b + chunk(first_row + j * RPI), dst + j * 1024u);
+                }
+            } else {
+#pragma unroll 1
+                for (int j = 0; j < N_DMA; ++j) {
+                    const int r = clamped(first_row + j * RPI, r0, r1);
+                    fetch_row(base, at, r, (uint32_t)r * row_b + chunk(first_row + j * RPI), dst + j * 1024u);
+                }
+            }
+        }
+    }
+};
+
+// Operand addresses in LDS, for a K tile at k0 and a V tile at v0 (see attention_bf16.hip).
+template <int D>
+struct Operands {
+    uint32_t k[D / 16], v[2][D / 32];
+    __device__ Operands(uint32_t k0, uint32_t v0, int lane) {
+        const int col = lane & 31, hh = lane >> 5;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) k[ks] = k0 + (uint32_t)(col * D + (((ks * 2 + hh) ^ swz<D>(col)) * 8)) * 2u;
+        const int gq = lane >> 4, i16 = lane & 15, qd = i16 & 3, jk = i16 >> 2;
+        const int cl = (gq & 1) * 2 + (qd >> 1), half = qd & 1;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int keyl = r * 8 + hh * 4 + jk;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) v[r][db] = v0 + (uint32_t)(keyl * D + (((db * 4 + cl) ^ swz<D>(keyl)) * 8) + half * 4) * 2u;
+        }
+    }
+    __device__ void load_k(uint32_t stage_b, bf16x8 (&kf)[D / 16]) const {
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) kf[ks] = *reinterpret_cast<LDS_AS const bf16x8*>(k[ks] + stage_b);
+    }
+    __device__ void load_v(uint32_t stage_b, int g16, bf16x8 (&vf)[D / 32]) const {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+            const tr4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(reinterpret_cast<LDS_AS tr4_t*>(v[0][db] + stage_b + g16 * 16 * D * 2));
+            const tr4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(reinterpret_cast<LDS_AS tr4_t*>(v[1][db] + stage_b + g16 * 16 * D * 2));
+            vf[db] = __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+};
+
+// A wavefront's 32 rows (a query per lane pair): the running softmax and output.
+template <int D>
+struct Rows {
+    bf16x8 qf[D / 16];
+    f32x16 o[D / 32];
+    float m_ref, l, sc;
+    int pos;                // index of this row's token
+    bool ok;
+    int64_t q_row;          // over (token, head)
+
+    __device__ Rows(const PagedProblem& p, const Job& job, int row, int kvh, int G, int hh) {
+        ok = row < job.n_rows;
+        const int tok = row / G;
+        pos = job.p0 + tok;
+        sc = p.scale * 1.4426950408889634f;
+        m_ref = -INFINITY;
+        l = 0.f;
+        q_row = (int64_t)(job.token0 + tok) * p.n_q_heads + kvh * G + (row - tok * G);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            u32x4 v = {0u, 0u, 0u, 0u};
+            if (ok) v = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(p.q) + q_row * D + ks * 16 + hh * 8);
+            qf[ks] = __builtin_bit_cast(bf16x8, v);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    }
+    __device__ __attribute__((always_inline)) void qk(const bf16x8 (&kf)[D / 16], f32x16& s) const {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
+    }
+    __device__ __attribute__((always_inline)) void mask(const PagedProblem& p, const Tiles<BN>& tiles, int t, int hh, f32x16& s) const {
+        const int k0 = tiles.key0(t) + hh * 4;
+        const Seen sees = tiles.in_prefix(t) ? Seen{0, tiles.n_prefix, 0} : seen_by(p, pos);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[j] = sees(k0 + (j >> 2) * 8 + (j & 3)) ? s[j] : -INFINITY;
+    }
+    // The running maximum over a tile's scores (lazily: O is rescaled when it has moved by more than 2^8); returns what the
+    // exponents refer to.
+    __device__ __attribute__((always_inline)) float maximum(const f32x16& s) {
+        float mx = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[j]);
+        mx = pair_max(mx);
+        const float mt2 = mx * sc;
+        if (__builtin_amdgcn_ballot_w64(mt2 > m_ref + RESCALE_GAP) != 0) {
+            const float m_new = fmaxf(m_ref, mt2);
+            const float alpha = (m_new == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m_ref - m_new);
+            l *= alpha;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[i][j] *= alpha;
+            m_ref = m_new;
+        }
+        return (m_ref == -INFINITY) ? 0.f : m_ref;
+    }
+    // Half a tile's probabilities, summed and rounded to bf16 for the product with V.
+    __device__ __attribute__((always_inline)) bf16x8 probabilities(const f32x16& s, int g16, float mr) {
+        bf16x8 pf;
+        float e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g16 * 8 + j], sc, -mr));
+            l += e[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const bf16x2 b2 = __builtin_convertvector((f32x2{e[j], e[j + 1]}), bf16x2);
+            pf[j] = b2[0];
+            pf[j + 1] = b2[1];
+        }
+        return pf;
+    }
+    __device__ __attribute__((always_inline)) void pv(const bf16x8 (&vf)[D / 32], const bf16x8& pf) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db], pf, o[db], 0, 0, 0);
+    }
+
+    // The values that drop_nonfinite took out of tiles [t0, t1), for the rows that do see them: from memory, key by key.
+    __device__ __attribute__((always_inline)) void add_nonfinite(const PagedProblem& p, const Job& job, const Tiles<BN>& tiles, int t0, int t1, int kvh, int hh) {
+        if (!ok) return;
+        const float mr = (m_ref == -INFINITY) ? 0.f : m_ref;
+        const int page = (int)p.b.by_page.d;
+        const bf16_t* qr = static_cast<const bf16_t*>(p.q) + q_row * D;
+#pragma unroll 1
+        for (int t = t0; t < t1; ++t) {
+            if (tiles.whole(t)) continue;
+            const bool pre = tiles.in_prefix(t);
+            const int32_t* table = pre ? p.prefix_pages : job.table;
+            const Seen sees = pre ? Seen{0, tiles.n_prefix, 0} : seen_by(p, pos);
+#pragma unroll 1
+            for (int key = tiles.key0(t); key < tiles.key0(t) + BN; ++key) {
+                if (!sees(key)) continue;
+                const int slot = (int)quot((uint32_t)key, p.b.by_page);
+                const int64_t row = (int64_t)clamped(table[slot], 0, p.b.n_pages - 1) * page + (key - slot * page);
+                const int64_t at = (row * p.n_kv_heads + kvh) * D;
+                const bf16_t* kr = static_cast<const bf16_t*>(p.b.k_pages) + at;
+                const bf16_t* vr = static_cast<const bf16_t*>(p.b.v_pages) + at;
+                float s = 0.f;
+#pragma unroll 1
+                for (int d = 0; d < D; ++d) s = fmaf((float)kr[d], (float)qr[d], s);
+                const float e = __builtin_amdgcn_exp2f(fmaf(s, sc, -mr));
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        const bf16x4 v = *reinterpret_cast<const bf16x4*>(vr + db * 32 + j * 2 + hh * 4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = (float)v[i];
+                            o[db][j + i] = fmaf(e, __builtin_fabsf(x) < INFINITY ? 0.f : x, o[db][j + i]);
+                        }
+                    }
+            }
+        }
+    }
+};
+
+// A tile that not every row sees whole: probabilities of 0 keep a value out only if it is finite, so the V tile's infinities and NaNs
+// become 0 in LDS.  Every wavefront that reads the tile calls this itself, before it reads; true if it found any.
+template <int D>
+__device__ inline bool drop_nonfinite(uint32_t v_tile, int lane) {
+    constexpr uint32_t TILE_B = BN * D * 2;
+    const uint32_t at = v_tile + lane * 16u;
+    uint32_t any = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < TILE_B; i += 1024) {
+        const u32x4 w = *reinterpret_cast<LDS_AS const u32x4*>(at + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) any |= (w[k] & 0x7f807f80u) + 0x00800080u;      // bit 15 of a half: its exponent is all ones
+    }
+    if (__builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0) == 0) return false;
+#pragma unroll 1
+    for (uint32_t i = 0; i < TILE_B; i += 1024) {
+        u32x4 w = *reinterpret_cast<LDS_AS const u32x4*>(at + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
+            if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0x0000ffffu;
+        }
+        *reinterpret_cast<LDS_AS u32x4*>(at + i) = w;
+    }
+    return true;
+}
+
+// The tiles [begin, end) of split `job.split`.
+__device__ inline void split_range(const PagedArgs& a, const Job& job, int n_tiles, int* begin, int* end) {
+    int n = (n_tiles + job.n_splits - 1) / job.n_splits;
+    n = n > a.min_tiles ? n : a.min_tiles;
+    *begin = job.split * n;
+    *end = *begin + n < n_tiles ? *begin + n : n_tiles;
+}
+template <int ROWS>
+__device__ inline Tiles<BN> tiles_of(const PagedProblem& p, const Job& job, int G) {
+    const int n_tok = job.n_rows / G, last = (job.row0 + ROWS - 1) / G;
+    return Tiles<BN>(p, job, job.row0 / G, last < n_tok ? last : n_tok - 1);
+}
+
+__device__ inline void store4(bf16_t* to, f32x4 v) {
+    u32x2 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2], v[3]}), bf16x2));
+    *reinterpret_cast<u32x2*>(to) = w;
+}
+
 template <int N>
 __device__ inline void step_barrier() {
     __builtin_amdgcn_sched_barrier(0);
@@ -37,282 +374,52 @@ __device__ inline void step_barrier() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// As dma16 (attention_mfma.h), from a 64-bit address per lane.
-__device__ inline void dma16_at(uint64_t addr, uint32_t lds_addr) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-                 ::"v"(addr), "s"(__builtin_amdgcn_readfirstlane(lds_addr)) : "memory", "m0");
-}
-
-// Page numbers of a tile's first key and of the page after it.
-struct Entries {
-    int32_t a, b;
-};
-// A tile in the pages: byte offsets (from k_pages or v_pages) of its row 0 as the first page has it and as the next one would,
-// and how many rows lie in the first.
-struct Place {
-    int64_t a, b;
-    int rows_a;
-    bool whole;             // all rows see the tile whole
-};
-
-// TWO_PAGES: 32 keys from a multiple of 32 on lie in two pages at most (pages of 32 tokens or more, or of 16); otherwise every
-// lane looks its rows' pages up.
+// A block of 128 rows: its four wavefronts share the tiles.  Order of a step, stages and operand reads as in attention_bf16.hip.
 template <int D, bool TWO_PAGES>
-__global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) {
-    constexpr int CH = D / 8;                 // 16-byte chunks per key row
-    constexpr int RPI = 64 / CH;              // key rows one 1 KB wave-wide load covers
-    constexpr int N_DMA = BN / RPI / WAVES;   // such loads per wave, tile and tensor
-    constexpr uint32_t TILE_B = BN * D * 2;
-    __shared__ __attribute__((aligned(1024))) bf16_t lds[2 * STAGES * BN * D];
-    __shared__ int sh_dropped;
-
+__device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, const Job& job, int kvh, uint32_t lds0, int* sh_dropped) {
+    typedef Source<D, TWO_PAGES, WAVES, false> Src;
+    constexpr uint32_t TILE_B = Src::TILE_B, VB = STAGES * TILE_B;
     const PagedProblem& p = a.p;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int col = lane & 31, hh = lane >> 5;
     const int G = p.n_q_heads / p.n_kv_heads;
-
-    // KV heads fastest: workgroups are dealt to the eight XCDs in turn, so that one of them sees few heads' keys
-    const int L = blockIdx.x / p.n_kv_heads, kvh = blockIdx.x - L * p.n_kv_heads;
-    Job job;
-    if (!find_job<BM>(p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)) return;
-
-    const int row = job.row0 + wave * WM + col;
-    const bool row_ok = row < job.n_rows;
-    const int tok = row / G;
-    const int first_tok = job.row0 / G;
-    int last_tok = (job.row0 + BM - 1) / G;
-    const int n_tok = job.n_rows / G;
-    last_tok = last_tok < n_tok ? last_tok : n_tok - 1;
     const bool wave_active = job.row0 + wave * WM < job.n_rows;
-    const Tiles<BN> tiles(p, job, first_tok, last_tok);
-    int per_split = (tiles.n + job.n_splits - 1) / job.n_splits;
-    per_split = per_split > a.min_tiles ? per_split : a.min_tiles;
-    const int t_begin = job.split * per_split;
-    const int t_end = t_begin + per_split < tiles.n ? t_begin + per_split : tiles.n;
-    const int pos = job.p0 + tok;                                       // this row's token: its index, the keys below it
-    const int row_hi = clamped(pos + 1, 0, p.b.capacity);
+    const Tiles<BN> tiles = tiles_of<BM>(p, job, G);
+    int t_begin, t_end;
+    split_range(a, job, tiles.n, &t_begin, &t_end);
+    const Src src(p, job, tiles, t_end, kvh, lane, wave);
+    const Operands<D> at(lds0, lds0 + VB, lane);
+    Rows<D> r(p, job, job.row0 + wave * WM + (lane & 31), kvh, G, hh);
 
-    const uint32_t row_b = (uint32_t)p.n_kv_heads * D * 2u;             // bytes of a token's keys
-    const char* k_base = static_cast<const char*>(p.b.k_pages) + kvh * D * 2;
-    const char* v_base = static_cast<const char*>(p.b.v_pages) + kvh * D * 2;
-    const int page = (int)p.b.by_page.d;
-
-    // ---- lane-constant addressing, as in attention_bf16.hip
-    const uint32_t lds0 = lds_addr_of(lds);
-    const int dma_row = wave * N_DMA * RPI + lane / CH;
-    const int dma_p = lane % CH;
-    uint32_t dma_coff[N_DMA], dma_off[N_DMA];
-#pragma unroll
-    for (int j = 0; j < N_DMA; ++j) {
-        dma_coff[j] = (uint32_t)(dma_p ^ swz<D>(dma_row + j * RPI)) * 16u;
-        dma_off[j] = (uint32_t)(dma_row + j * RPI) * row_b + dma_coff[j];
-    }
-    const uint32_t dma_lds = lds0 + (uint32_t)(wave * N_DMA) * 1024u;
-    uint32_t k_addr[D / 16];
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-        k_addr[ks] = lds0 + (uint32_t)(col * D + (((ks * 2 + hh) ^ swz<D>(col)) * 8)) * 2u;
-    uint32_t v_addr[2][D / 32];
-    {
-        const int gq = lane >> 4, i16 = lane & 15, qd = i16 & 3, jk = i16 >> 2;
-        const int cl = (gq & 1) * 2 + (qd >> 1), half = qd & 1;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int keyl = r * 8 + hh * 4 + jk;
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db)
-                v_addr[r][db] = lds0 + STAGES * TILE_B + (uint32_t)(keyl * D + (((db * 4 + cl) ^ swz<D>(keyl)) * 8) + half * 4) * 2u;
-        }
-    }
-
-    // ---- pages
-    auto table_of = [&](int t) { return tiles.in_prefix(t) ? p.prefix_pages : job.table; };
-    auto last_slot_of = [&](int t) {
-        return tiles.in_prefix(t) ? (int)quot((uint32_t)(tiles.n_prefix - 1), p.b.by_page) : p.b.max_pages - 1;
+    Places places;
+    Place at_k, at_v;                        // of tiles t + 4 and t + 3 in step t
+    uint32_t whole = 0;                      // bit i: all rows see tile t + i whole
+    auto fetch = [&](int t, uint32_t kl, uint32_t vl) __attribute__((always_inline)) {      // the loads of step t
+        at_v = at_k;
+        at_k = src.place(places, src.in_list(t + 4));
+        src.fetch(src.k_base, src.in_list(t + 4), at_k, lds0 + kl);
+        src.fetch(src.v_base, src.in_list(t + 3), at_v, lds0 + VB + vl);
     };
-    auto in_list = [&](int t) { return t < t_end ? t : t_end - 1; };
-    auto entries = [&](int t) {              // t is in the list
-        const int slot = (int)quot((uint32_t)tiles.key0(t), p.b.by_page), last = last_slot_of(t);
-        const int32_t* table = table_of(t);
-        return Entries{scalar_word(table, slot), scalar_word(table, slot < last ? slot + 1 : last)};
-    };
-    auto place = [&](int t, Entries e) {
-        const int k0 = tiles.key0(t), within = k0 - (int)quot((uint32_t)k0, p.b.by_page) * page;
-        const int pa = clamped(e.a, 0, p.b.n_pages - 1), pb = clamped(e.b, 0, p.b.n_pages - 1);
-        return Place{((int64_t)pa * page + within) * row_b, ((int64_t)pb * page + within - page) * row_b, page - within, tiles.whole(t, 1)};
-    };
-    // Row r of a tile, by the page it lies in: lanes of either page take a load of their own, from a uniform address (where a
-    // load has lanes of both, one more is in flight than step_barrier counts, which only makes it wait longer).
-    auto dma_row_of = [&](const char* base, const Place& at, int r, uint32_t off, uint32_t dst) {
-        if (r < at.rows_a) dma16<false>(base + at.a, off, dst);
-        else dma16<false>(base + at.b, off, dst);
-    };
-    // Tile t; the rows that no row of the block sees repeat the nearest that one does.
-    auto dma_tile = [&](const char* base, int t, const Place& at, uint32_t stage_b) {
-        if (TWO_PAGES) {
-            if (at.whole && at.rows_a >= BN) {
-#pragma unroll
-                for (int j = 0; j < N_DMA; ++j) dma16<false>(base + at.a, dma_off[j], dma_lds + stage_b + j * 1024u);
-                return;
-            }
-            int r0 = 0, r1 = BN - 1;
-            if (!at.whole) tiles.rows(t, &r0, &r1);
-#pragma unroll
-            for (int j = 0; j < N_DMA; ++j) {
-                const int r = clamped(dma_row + j * RPI, r0, r1);
-                dma_row_of(base, at, r, (uint32_t)r * row_b + dma_coff[j], dma_lds + stage_b + j * 1024u);
-            }
-        } else {
-            const int32_t* table = table_of(t);
-            const int k0 = tiles.key0(t);
-            int r0, r1;
-            tiles.rows(t, &r0, &r1);
-            uint64_t from[N_DMA];
-#pragma unroll
-            for (int j = 0; j < N_DMA; ++j) {
-                const int key = k0 + clamped(dma_row + j * RPI, r0, r1), slot = (int)quot((uint32_t)key, p.b.by_page);
-                const int pg = clamped(table[slot], 0, p.b.n_pages - 1);
-                from[j] = reinterpret_cast<uint64_t>(base) + (uint64_t)((int64_t)pg * page + (key - slot * page)) * row_b + dma_coff[j];
-            }
-#pragma unroll
-            for (int j = 0; j < N_DMA; ++j) dma16_at(from[j], dma_lds + stage_b + j * 1024u);
-        }
-    };
-    constexpr int DMA_PER_STEP = 2 * N_DMA;
-
-    bf16x8 qf[D / 16];
-    const int64_t q_row = (int64_t)(job.token0 + tok) * p.n_q_heads + kvh * G + (row - tok * G);     // over (token, head)
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-        u32x4 v = {0u, 0u, 0u, 0u};
-        if (row_ok) v = *reinterpret_cast<const u32x4*>(static_cast<const bf16_t*>(p.q) + q_row * D + ks * 16 + hh * 8);
-        qf[ks] = __builtin_bit_cast(bf16x8, v);
-    }
-
-    f32x16 o[D / 32];
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
-    float m_ref = -INFINITY, l_part = 0.f;
-    const float sc = p.scale * 1.4426950408889634f;
-
-    auto qk = [&](const bf16x8 (&kf)[D / 16], f32x16& s) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[j] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
-    };
-    auto load_k = [&](uint32_t stage_b, bf16x8 (&kf)[D / 16]) {
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) kf[ks] = *reinterpret_cast<LDS_AS const bf16x8*>(k_addr[ks] + stage_b);
-    };
-
-    // Entries of tile t + 5 and places of tiles t + 4 and t + 3, as step t needs them.
-    Entries e_next;
-    Place at_k, at_v;
-
-    // A tile that not every row sees whole: probabilities of 0 keep a value out only if it is finite, so its infinities and NaNs
-    // become 0 in LDS (every wavefront sees to that for itself, before it reads the tile) and are added after the loop.
-    auto drop_nonfinite = [&](uint32_t stage_b) {
-        const uint32_t at = lds0 + STAGES * TILE_B + stage_b + lane * 16u;
-        uint32_t any = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < TILE_B; i += 1024) {
-            const u32x4 w = *reinterpret_cast<LDS_AS const u32x4*>(at + i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) any |= (w[k] & 0x7f807f80u) + 0x00800080u;      // bit 15 of a half: its exponent is all ones
-        }
-        if (__builtin_amdgcn_ballot_w64((any & 0x80008000u) != 0) == 0) return;
-        sh_dropped = 1;
-#pragma unroll 1
-        for (uint32_t i = 0; i < TILE_B; i += 1024) {
-            u32x4 w = *reinterpret_cast<LDS_AS const u32x4*>(at + i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if ((w[k] & 0x7f80u) == 0x7f80u) w[k] &= 0xffff0000u;
-                if ((w[k] & 0x7f800000u) == 0x7f800000u) w[k] &= 0x0000ffffu;
-            }
-            *reinterpret_cast<LDS_AS u32x4*>(at + i) = w;
-        }
-    };
-
-    // One step, as in attention_bf16.hip.
+    constexpr int DMA_PER_STEP = 2 * Src::N_DMA;
     auto step = [&](int t, f32x16& s_cur, f32x16& s_next, auto kn, auto kl, auto vc, auto vl) __attribute__((always_inline)) {
         constexpr uint32_t KN = decltype(kn)::value * TILE_B, KL = decltype(kl)::value * TILE_B;
         constexpr uint32_t VC = decltype(vc)::value * TILE_B, VL = decltype(vl)::value * TILE_B;
-        if (TWO_PAGES) {
-            at_v = at_k;
-            at_k = place(in_list(t + 4), e_next);
+        fetch(t, KL, VL);
+        if (!(whole & 1)) {
+            r.mask(p, tiles, t, hh, s_cur);
+            if (drop_nonfinite<D>(lds0 + VB + VC, lane)) *sh_dropped = 1;
         }
-        dma_tile(k_base, in_list(t + 4), at_k, KL);
-        dma_tile(v_base, in_list(t + 3), at_v, STAGES * TILE_B + VL);
-        if (TWO_PAGES) e_next = entries(in_list(t + 5));
-        if (!tiles.whole(t, 1)) {
-            const int k0 = tiles.key0(t);
-            const bool pre = tiles.in_prefix(t);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int key = k0 + (j >> 2) * 8 + hh * 4 + (j & 3);
-                s_cur[j] = (pre ? key < tiles.n_prefix : sees(p, pos, row_hi, key)) ? s_cur[j] : -INFINITY;
-            }
-            drop_nonfinite(VC);
-        }
-        bf16x8 kf[D / 16];
-        load_k(KN, kf);
-        bf16x8 vf[2][D / 32];
-        auto load_v = [&](int g16) {
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
-                const tr4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                    reinterpret_cast<LDS_AS tr4_t*>(v_addr[0][db] + VC + g16 * 16 * D * 2));
-                const tr4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-                    reinterpret_cast<LDS_AS tr4_t*>(v_addr[1][db] + VC + g16 * 16 * D * 2));
-                vf[g16][db] = __builtin_shufflevector(__builtin_bit_cast(bf16x4, lo),
-                                                      __builtin_bit_cast(bf16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
-            }
-        };
-        load_v(0);
+        whole = (whole >> 1) | ((uint32_t)at_k.whole << 3);
+        bf16x8 kf[D / 16], vf[2][D / 32];
+        at.load_k(KN, kf);
+        at.load_v(VC, 0, vf[0]);
         __builtin_amdgcn_sched_barrier(0);
-        float mx = s_cur[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s_cur[j]);
-        mx = pair_max(mx);
-        const float mt2 = mx * sc;
-        if (__builtin_amdgcn_ballot_w64(mt2 > m_ref + RESCALE_GAP) != 0) {
-            const float m_new = fmaxf(m_ref, mt2);
-            const float alpha = (m_new == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(m_ref - m_new);
-            l_part *= alpha;
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) o[i][j] *= alpha;
-            m_ref = m_new;
-        }
-        const float mr = (m_ref == -INFINITY) ? 0.f : m_ref;
+        const float mr = r.maximum(s_cur);
         __builtin_amdgcn_s_setprio(3);
-        qk(kf, s_next);            // past the last tile this works on a stale stage and is unused
-        load_v(1);
+        r.qk(kf, s_next);            // past the last tile this works on a stale stage and is unused
+        at.load_v(VC, 1, vf[1]);
 #pragma unroll
-        for (int g16 = 0; g16 < 2; ++g16) {
-            float e[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                e[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(s_cur[g16 * 8 + j], sc, -mr));
-                l_part += e[j];
-            }
-            bf16x8 pf;
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const bf16x2 b2 = __builtin_convertvector((f32x2{e[j], e[j + 1]}), bf16x2);
-                pf[j] = b2[0];
-                pf[j + 1] = b2[1];
-            }
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db)
-                o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[g16][db], pf, o[db], 0, 0, 0);
-        }
+        for (int g16 = 0; g16 < 2; ++g16) r.pv(vf[g16], r.probabilities(s_cur, g16, mr));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -324,22 +431,22 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
     };
 
     if (t_begin < t_end) {
-        if (tid == 0) sh_dropped = 0;        // before the first barrier
+        if (tid == 0) *sh_dropped = 0;       // before the first barrier
         f32x16 s_a, s_b;
-        constexpr uint32_t VB = STAGES * TILE_B;
-#pragma unroll
+        src.fill(places, t_begin);
+#pragma unroll 1
         for (int i = 0; i < 4; ++i) {        // K of four tiles, V of three
-            const int t = in_list(t_begin + i);
-            if (TWO_PAGES) at_k = place(t, entries(t));
-            dma_tile(k_base, t, at_k, i * TILE_B);
-            if (i < 3) dma_tile(v_base, t, at_k, VB + i * TILE_B);
+            const int t = src.in_list(t_begin + i);
+            at_k = src.place(places, t);
+            whole |= (uint32_t)at_k.whole << i;
+            src.fetch(src.k_base, t, at_k, lds0 + i * TILE_B);
+            if (i < 3) src.fetch(src.v_base, t, at_k, lds0 + VB + i * TILE_B);
         }
-        if (TWO_PAGES) e_next = entries(in_list(t_begin + 4));
         step_barrier<0>();
         if (wave_active) {
             bf16x8 kf0[D / 16];
-            load_k(0, kf0);
-            qk(kf0, s_a);
+            at.load_k(0, kf0);
+            r.qk(kf0, s_a);
         }
         step_barrier<0>();
         wait_vmem();                         // the Q fragments have landed, as the compiler sees it
@@ -347,13 +454,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
         if (!wave_active) {
             for (; t < t_end; ++t) {         // the same loads into the same stages as the steps below
                 const uint32_t i4 = (uint32_t)(t - t_begin) & 3u;
-                if (TWO_PAGES) {
-                    at_v = at_k;
-                    at_k = place(in_list(t + 4), e_next);
-                }
-                dma_tile(k_base, in_list(t + 4), at_k, i4 * TILE_B);
-                dma_tile(v_base, in_list(t + 3), at_v, VB + ((i4 + 3u) & 3u) * TILE_B);
-                if (TWO_PAGES) e_next = entries(in_list(t + 5));
+                fetch(t, i4 * TILE_B, ((i4 + 3u) & 3u) * TILE_B);
                 step_barrier<2 * DMA_PER_STEP>();
             }
         }
@@ -368,76 +469,170 @@ __global__ __launch_bounds__(WAVES * 64, 2) void attn_paged_kernel(PagedArgs a) 
             ++t;
         }
         wait_vmem();               // no load may still be writing LDS when the workgroup retires
+        // (a step's last barrier is behind every write of the flag)
+        if (*sh_dropped != 0) r.add_nonfinite(p, job, tiles, t_begin, t_end, kvh, hh);
     }
 
-    // The values left out, for the rows that do see them: from memory, key by key.  (A step's last barrier is behind every write.)
-    if (t_begin < t_end && sh_dropped != 0 && row_ok) {
-        const float mr = (m_ref == -INFINITY) ? 0.f : m_ref;
-        const bf16_t* qr = static_cast<const bf16_t*>(p.q) + q_row * D;
-#pragma unroll 1
-        for (int t = t_begin; t < t_end; ++t) {
-            if (tiles.whole(t, 1)) continue;
-            const bool pre = tiles.in_prefix(t);
-            const int32_t* table = table_of(t);
-#pragma unroll 1
-            for (int key = tiles.key0(t); key < tiles.key0(t) + BN; ++key) {
-                if (!(pre ? key < tiles.n_prefix : sees(p, pos, row_hi, key))) continue;
-                const int slot = (int)quot((uint32_t)key, p.b.by_page);
-                const int pg = clamped(table[slot], 0, p.b.n_pages - 1);
-                const int64_t at = ((int64_t)pg * page + (key - slot * page)) * row_b;
-                const bf16_t* kr = reinterpret_cast<const bf16_t*>(k_base + at);
-                const bf16_t* vr = reinterpret_cast<const bf16_t*>(v_base + at);
-                float s = 0.f;
-#pragma unroll 1
-                for (int d = 0; d < D; ++d) s = fmaf((float)kr[d], (float)qr[d], s);
-                const float e = __builtin_amdgcn_exp2f(fmaf(s, sc, -mr));
-#pragma unroll
-                for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const float v = (float)vr[db * 32 + (j >> 2) * 8 + hh * 4 + (j & 3)];
-                        if (!(__builtin_fabsf(v) < INFINITY)) o[db][j] = fmaf(e, v, o[db][j]);
-                    }
-            }
-        }
-    }
-
-    const float l_tot = pair_sum(l_part);
-    if (!row_ok) return;
+    const float l_tot = pair_sum(r.l);
+    if (!r.ok) return;
     if (a.n_slots == 1) {
         const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;      // a row that sees nothing: zeros
-        bf16_t* orow = static_cast<bf16_t*>(p.out) + q_row * D;
+        bf16_t* out = static_cast<bf16_t*>(p.out) + r.q_row * D + hh * 4;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-            for (int j4 = 0; j4 < 4; ++j4) {
-                u32x2 w;
-                w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[db][j4 * 4] * inv, o[db][j4 * 4 + 1] * inv}), bf16x2));
-                w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{o[db][j4 * 4 + 2] * inv, o[db][j4 * 4 + 3] * inv}), bf16x2));
-                *reinterpret_cast<u32x2*>(orow + db * 32 + j4 * 8 + hh * 4) = w;
-            }
+            for (int j = 0; j < 16; j += 4)
+                store4(out + db * 32 + j * 2, f32x4{r.o[db][j] * inv, r.o[db][j + 1] * inv, r.o[db][j + 2] * inv, r.o[db][j + 3] * inv});
     } else {
-        const int64_t at = (int64_t)job.slot * p.b.n_tokens * p.n_q_heads + q_row;
+        const int64_t to = (int64_t)job.slot * p.b.n_tokens * p.n_q_heads + r.q_row;
+        float* out = a.part_o + to * D + hh * 4;
         if (l_tot != 0.f) {
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-                for (int j4 = 0; j4 < 4; ++j4)
-                    *reinterpret_cast<f32x4*>(a.part_o + at * D + db * 32 + j4 * 8 + hh * 4) =
-                        f32x4{o[db][j4 * 4], o[db][j4 * 4 + 1], o[db][j4 * 4 + 2], o[db][j4 * 4 + 3]};
+                for (int j = 0; j < 16; j += 4)
+                    *reinterpret_cast<f32x4*>(out + db * 32 + j * 2) = f32x4{r.o[db][j], r.o[db][j + 1], r.o[db][j + 2], r.o[db][j + 3]};
         }
-        if (hh == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{l_tot != 0.f ? m_ref : -INFINITY, l_tot};
+        if (hh == 0) *reinterpret_cast<f32x2*>(a.part_ml + to * 2) = f32x2{l_tot != 0.f ? r.m_ref : -INFINITY, l_tot};
     }
+}
+
+// A block of 32 rows, as a decode step's: its four wavefronts divide the KEYS, each walks its run of tiles through a K and a V tile
+// of its own in LDS without a barrier, and their results meet in LDS.  Nobody else reads the keys, so loads are non-temporal.
+template <int D, bool TWO_PAGES>
+__device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, const Job& job, int kvh, unsigned char* lds, f32x2 (*ml)[WM]) {
+    typedef Source<D, TWO_PAGES, 1, true> Src;
+    constexpr uint32_t TILE_B = Src::TILE_B;
+    constexpr int N_DMA = Src::N_DMA, CPR = D / 4;       // 16-byte fp32 chunks per output row
+    const PagedProblem& p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, hh = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int G = p.n_q_heads / p.n_kv_heads;
+    const Tiles<BN> tiles = tiles_of<WM>(p, job, G);
+    int begin, end;
+    split_range(a, job, tiles.n, &begin, &end);
+    const int n = end > begin ? end - begin : 0, each = n / WAVES, rest = n - each * WAVES;      // the first `rest` runs are one longer
+    const int t_begin = begin + each * wave + (wave < rest ? wave : rest), t_end = t_begin + each + (wave < rest);
+    const uint32_t k_tile = lds_addr_of(lds) + (uint32_t)wave * 2u * TILE_B, v_tile = k_tile + TILE_B;
+    const Src src(p, job, tiles, t_end, kvh, lane, 0);
+    Places places;
+    Place now, next;                         // of tiles t and t + 1
+    if (t_begin < t_end) {                   // the first tile's loads leave before anything else is set up
+        src.fill(places, t_begin);
+        now = src.place(places, t_begin);
+        src.fetch(src.k_base, t_begin, now, k_tile);
+        src.fetch(src.v_base, t_begin, now, v_tile);
+        next = src.place(places, src.in_list(t_begin + 1));
+    }
+    Rows<D> r(p, job, job.row0 + col, kvh, G, hh);
+    const Operands<D> at(k_tile, v_tile, lane);
+    wait_vmem();                             // the Q fragments have landed, as the compiler sees it
+    bool dropped = false;
+    auto reads_done = [] {                   // operands are in registers: their tile may be overwritten
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto wait_newest = [](auto k) { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(decltype(k)::value) : "memory"); };
+    for (int t = t_begin; t < t_end; ++t) {
+        const bool more = t + 1 < t_end;
+        wait_newest(IC<N_DMA>{});            // K(t); V(t)'s loads are the only newer ones
+        bf16x8 kf[D / 16], vf[2][D / 32];
+        f32x16 s;
+        at.load_k(0, kf);
+        reads_done();
+        if (more) src.fetch(src.k_base, t + 1, next, k_tile);
+        r.qk(kf, s);
+        const bool whole = now.whole;
+        if (!whole) r.mask(p, tiles, t, hh, s);
+        const float mr = r.maximum(s);
+        const bf16x8 p0 = r.probabilities(s, 0, mr), p1 = r.probabilities(s, 1, mr);
+        if (more) wait_newest(IC<N_DMA>{});  // V(t); K(t+1)'s loads are newer
+        else wait_newest(IC<0>{});
+        if (!whole) dropped |= drop_nonfinite<D>(v_tile, lane);
+        at.load_v(0, 0, vf[0]);
+        at.load_v(0, 1, vf[1]);
+        reads_done();
+        if (more) {
+            src.fetch(src.v_base, t + 1, next, v_tile);
+            now = next;
+            next = src.place(places, src.in_list(t + 2));
+        }
+        r.pv(vf[0], p0);
+        r.pv(vf[1], p1);
+    }
+    if (dropped) r.add_nonfinite(p, job, tiles, t_begin, t_end, kvh, hh);
+
+    // ---- the wavefronts' results meet in LDS, each scaled to the common maximum, in its own tiles; 16-byte chunk c of row i lies at
+    // chunk position c ^ i, so that writes (a row per lane) and reads (a row per CPR lanes) touch all banks
+    const float l_tot = pair_sum(r.l);
+    if (hh == 0) ml[wave][col] = f32x2{l_tot != 0.f ? r.m_ref : -INFINITY, l_tot};
+    __syncthreads();
+    const int n_rows = job.n_rows - job.row0 < WM ? job.n_rows - job.row0 : WM;
+    if (r.ok) {
+        float m_all = ml[0][col][0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m_all = fmaxf(m_all, ml[w][col][0]);
+        const float f = l_tot == 0.f ? 0.f : __builtin_amdgcn_exp2f(r.m_ref - m_all);
+        f32x4* mine = reinterpret_cast<f32x4*>(lds + (size_t)wave * 2 * TILE_B);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int j4 = 0; j4 < 4; ++j4) {
+                const int c = db * 8 + j4 * 2 + hh;
+                mine[col * CPR + (c ^ (col & (CPR - 1)))] =
+                    f32x4{r.o[db][j4 * 4] * f, r.o[db][j4 * 4 + 1] * f, r.o[db][j4 * 4 + 2] * f, r.o[db][j4 * 4 + 3] * f};
+            }
+    }
+    __syncthreads();
+    for (int e = tid; e < n_rows * CPR; e += THREADS) {
+        const int i = e / CPR, c = e % CPR, row = job.row0 + i, tok = row / G;
+        const int64_t q_row = (int64_t)(job.token0 + tok) * p.n_q_heads + kvh * G + (row - tok * G);
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4*>(lds + (size_t)w * 2 * TILE_B + (i * CPR + (c ^ (i & (CPR - 1)))) * 16);
+        float m_all = ml[0][i][0], l_all = 0.f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m_all = fmaxf(m_all, ml[w][i][0]);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+            if (ml[w][i][1] != 0.f) l_all += ml[w][i][1] * __builtin_amdgcn_exp2f(ml[w][i][0] - m_all);
+        if (a.n_slots == 1) {
+            store4(static_cast<bf16_t*>(p.out) + q_row * D + c * 4, v * (l_all == 0.f ? 0.f : 1.f / l_all));
+        } else {
+            const int64_t to = (int64_t)job.slot * p.b.n_tokens * p.n_q_heads + q_row;
+            if (l_all != 0.f) *reinterpret_cast<f32x4*>(a.part_o + to * D + c * 4) = v;
+            if (c == 0) *reinterpret_cast<f32x2*>(a.part_ml + to * 2) = f32x2{m_all, l_all};
+        }
+    }
+}
+
+// FEW: the sequences' own keys by blocks of 32 rows, a prefix shared by the batch still by blocks of 128.
+template <int D, bool TWO_PAGES, bool FEW>
+__global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGES * BN * D * 2];
+    __shared__ f32x2 ml[FEW ? WAVES : 1][WM];
+    __shared__ int sh_dropped;
+    // KV heads fastest: workgroups are dealt to the eight XCDs in turn, so that one of them sees few heads' keys
+    const int L = blockIdx.x / a.p.n_kv_heads, kvh = blockIdx.x - L * a.p.n_kv_heads, lane = threadIdx.x & 63;
+    const bool prefix = L < a.prefix_blocks * a.prefix_splits;
+    Job job;
+    if (FEW && !prefix) {
+        if (find_own_job<WM>(a.p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)) keys_block<D, TWO_PAGES>(a, job, kvh, lds, ml);
+        return;
+    }
+    if (prefix ? find_prefix_job<BM>(a.p, a.prefix_blocks, a.prefix_splits, L, &job)
+               : find_own_job<BM>(a.p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job))
+        rows_block<D, TWO_PAGES>(a, job, kvh, lds_addr_of(lds), &sh_dropped);
 }
 
 // Joins the partial results of the rows (token, head).  TPR threads own four dimensions each of a row; the slots of a row are
 // spread over a.n_slots / per_group thread groups, whose sums meet in LDS, so that a few rows of many slots (one user) are not
 // read one after the other.  Slots of no keys hold the maximum -inf and are not read.
-constexpr int MERGE_THREADS = 256;
+constexpr int MOST_MERGE_THREADS = 1024;
 template <bool BF16>
-__global__ __launch_bounds__(MERGE_THREADS) void attn_paged_merge_kernel(PagedArgs a, int tpr, int groups, int rows_per_block) {
-    __shared__ float red_m[MERGE_THREADS], red_l[MERGE_THREADS];
-    __shared__ f32x4 red_o[MERGE_THREADS];
+__global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(PagedArgs a, int tpr, int groups, int rows_per_block) {
+    __shared__ float red_m[MOST_MERGE_THREADS], red_l[MOST_MERGE_THREADS];
+    __shared__ f32x4 red_o[MOST_MERGE_THREADS];
     const PagedProblem& p = a.p;
     const int D = p.head_dim, tid = threadIdx.x;
     const int unit = tid / tpr, dq = tid - unit * tpr;           // (row of the block, group), dimensions 4 dq ..
@@ -454,15 +649,14 @@ __global__ __launch_bounds__(MERGE_THREADS) void attn_paged_merge_kernel(PagedAr
             f32x2 ml[U];
             f32x4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u) {        // all loads leave together; what an empty slot holds is not used
                 const int s = s0 + u * groups;
                 ml[u] = f32x2{-INFINITY, 0.f};
-                v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (s < a.n_slots) ml[u] = *reinterpret_cast<const f32x2*>(a.part_ml + ((int64_t)s * n_rows + row) * 2);
+                if (s < a.n_slots) {
+                    ml[u] = *reinterpret_cast<const f32x2*>(a.part_ml + ((int64_t)s * n_rows + row) * 2);
+                    v[u] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)s * n_rows + row) * D + dq * 4);
+                }
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (ml[u][0] != -INFINITY) v[u] = *reinterpret_cast<const f32x4*>(a.part_o + ((int64_t)(s0 + u * groups) * n_rows + row) * D + dq * 4);
             float m_new = m;
 #pragma unroll
             for (int u = 0; u < U; ++u) m_new = fmaxf(m_new, ml[u][0]);
@@ -533,7 +727,9 @@ __global__ __launch_bounds__(F32_ROWS * 64) void attn_paged_f32_kernel(PagedArgs
     const int D = p.head_dim, G = p.n_q_heads / p.n_kv_heads;
     const int L = blockIdx.x / p.n_kv_heads, kvh = blockIdx.x - L * p.n_kv_heads;
     Job job;
-    if (!find_job<F32_ROWS>(p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)) return;
+    if (!(L < a.prefix_blocks * a.prefix_splits ? find_prefix_job<F32_ROWS>(p, a.prefix_blocks, a.prefix_splits, L, &job)
+                                                : find_own_job<F32_ROWS>(p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)))
+        return;
     const int row = job.row0 + wave;
     if (row >= job.n_rows) return;           // whole wavefront leaves; nothing below waits for the workgroup
     const int tok = row / G, pos = job.p0 + tok;
@@ -616,29 +812,43 @@ int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
 
 PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim, int64_t n_tokens, int64_t n_seqs, int64_t max_kv,
                           int64_t window, int64_t sinks, int64_t n_prefix) {
-    const int64_t G = n_q_heads / n_kv_heads;
+    const int64_t G = n_q_heads / n_kv_heads, all_rows = n_tokens * G;
+    const bool bf16 = dtype == REKV_BF16;
     PagedPlan plan;
-    plan.rows = dtype == REKV_BF16 ? BM : F32_ROWS;
-    plan.blocks = (int32_t)(n_tokens * G / plan.rows + n_seqs);
-    plan.min_tiles = 4;
-    const int64_t places = dtype == REKV_BF16 ? 512 : 1024;
-    auto splits_of = [&](int64_t blocks, int64_t keys) {
-        const int64_t most = keys / (BN * plan.min_tiles) > 1 ? keys / (BN * plan.min_tiles) : 1, s = places / (blocks * n_kv_heads);
-        return (int32_t)(s < 1 ? 1 : s < most ? s : most);
+    const bool few = bf16 && all_rows <= n_seqs * WM;
+    plan.rows = !bf16 ? F32_ROWS : few ? WM : BM;
+    const int64_t prefix_rows = bf16 ? BM : F32_ROWS;
+    plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
+    plan.min_tiles = few ? 8 : 4;
+    const int64_t places = bf16 ? 512 : 1024;
+    auto splits_of = [&](int64_t busy, int64_t keys, int64_t most_tiles) {
+        const int64_t tiles = up(keys, BN), most = tiles / plan.min_tiles;
+        int64_t s = places / (busy * n_kv_heads);
+        if (s < tiles / most_tiles) s = tiles / most_tiles;
+        return (int32_t)(s > most ? most < 1 ? 1 : most : s < 1 ? 1 : s);
     };
     plan.prefix_blocks = plan.prefix_splits = 0;
     int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
     // Rows that fill blocks by themselves walk the prefix in their own blocks.
-    const bool together = n_prefix > 0 && n_tokens * G < n_seqs * (plan.rows / 2);
+    const bool together = n_prefix > 0 && all_rows < n_seqs * (prefix_rows / 2);
     if (together) {
-        plan.prefix_blocks = (int32_t)up(n_tokens * G, plan.rows);
-        plan.prefix_splits = splits_of(plan.prefix_blocks, n_prefix);
+        plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
+        plan.prefix_splits = splits_of(plan.prefix_blocks, n_prefix, 1 << 30);
     } else {
         keys += n_prefix;
     }
-    plan.splits = splits_of(plan.blocks, keys);
+    const int64_t busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
+    plan.splits = splits_of(busy, keys, few ? 64 : 1 << 30);
     plan.workspace_bytes = plan.slots() > 1 ? n_tokens * n_q_heads * plan.slots() * (head_dim + 2) * 4 : 0;
     return plan;
+}
+
+template <int D>
+void launch_bf16(const PagedArgs& a, bool two_pages, bool few, dim3 grid, hipStream_t stream) {
+    if (two_pages && few) hipLaunchKernelGGL((attn_paged_kernel<D, true, true>), grid, dim3(THREADS), 0, stream, a);
+    else if (two_pages) hipLaunchKernelGGL((attn_paged_kernel<D, true, false>), grid, dim3(THREADS), 0, stream, a);
+    else if (few) hipLaunchKernelGGL((attn_paged_kernel<D, false, true>), grid, dim3(THREADS), 0, stream, a);
+    else hipLaunchKernelGGL((attn_paged_kernel<D, false, false>), grid, dim3(THREADS), 0, stream, a);
 }
 
 hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int dtype, void* workspace, hipStream_t stream) {
@@ -652,29 +862,19 @@ hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int d
     a.part_ml = a.n_slots > 1 ? a.part_o + rows * a.n_slots * p.head_dim : nullptr;
     const int64_t jobs = (int64_t)plan.prefix_blocks * plan.prefix_splits + (int64_t)plan.blocks * plan.splits;
     const dim3 grid((unsigned)(jobs * p.n_kv_heads));
-    const uint32_t page = p.b.by_page.d;
-    const bool two = page >= BN || page == 16;
-    if (dtype == REKV_F32)
-        hipLaunchKernelGGL(attn_paged_f32_kernel, grid, dim3(F32_ROWS * 64), 0, stream, a);
-    else if (p.head_dim == 128 && two)
-        hipLaunchKernelGGL((attn_paged_kernel<128, true>), grid, dim3(WAVES * 64), 0, stream, a);
-    else if (p.head_dim == 128)
-        hipLaunchKernelGGL((attn_paged_kernel<128, false>), grid, dim3(WAVES * 64), 0, stream, a);
-    else if (two)
-        hipLaunchKernelGGL((attn_paged_kernel<64, true>), grid, dim3(WAVES * 64), 0, stream, a);
-    else
-        hipLaunchKernelGGL((attn_paged_kernel<64, false>), grid, dim3(WAVES * 64), 0, stream, a);
+    const bool two_pages = p.b.by_page.d >= BN || p.b.by_page.d == 16;
+    if (dtype == REKV_F32) hipLaunchKernelGGL(attn_paged_f32_kernel, grid, dim3(F32_ROWS * 64), 0, stream, a);
+    else if (p.head_dim == 128) launch_bf16<128>(a, two_pages, plan.rows == WM, grid, stream);
+    else launch_bf16<64>(a, two_pages, plan.rows == WM, grid, stream);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_slots == 1) return e;
-    const int tpr = p.head_dim / 4, units = MERGE_THREADS / tpr;
+    const int tpr = p.head_dim / 4, threads = a.n_slots > 32 ? MOST_MERGE_THREADS : 256, units = threads / tpr;
     int groups = 1;                           // of at most four slots each, as far as a block has threads
     while (groups * 2 <= units && groups * 4 < a.n_slots) groups *= 2;
     const int per_block = units / groups;
     const dim3 merge_grid((unsigned)up(rows, per_block));
-    if (dtype == REKV_F32)
-        hipLaunchKernelGGL(attn_paged_merge_kernel<false>, merge_grid, dim3(MERGE_THREADS), 0, stream, a, tpr, groups, per_block);
-    else
-        hipLaunchKernelGGL(attn_paged_merge_kernel<true>, merge_grid, dim3(MERGE_THREADS), 0, stream, a, tpr, groups, per_block);
+    if (dtype == REKV_F32) hipLaunchKernelGGL(attn_paged_merge_kernel<false>, merge_grid, dim3(threads), 0, stream, a, tpr, groups, per_block);
+    else hipLaunchKernelGGL(attn_paged_merge_kernel<true>, merge_grid, dim3(threads), 0, stream, a, tpr, groups, per_block);
     return hipGetLastError();
 }
 

@@ -51,42 +51,44 @@ struct Job {
     bool own;               // whether it sees own keys
 };
 
-// Work of block `r` (over row blocks and splits, of one KV head): false if there is none.
+// Block r of a launch (of one KV head): first the prefix jobs, where the prefix is computed for the batch at once, then the own ones,
+// row blocks fastest.  False: no work.
 template <int ROWS>
-__device__ inline bool find_job(const PagedProblem& p, int prefix_blocks, int prefix_splits, int blocks, int splits, int r, int lane, Job* job) {
+__device__ inline bool find_prefix_job(const PagedProblem& p, int prefix_blocks, int prefix_splits, int r, Job* job) {
+    const int G = p.n_q_heads / p.n_kv_heads;
+    const TokenRange t = token_range(p.b);
+    job->split = job->slot = r / prefix_blocks;
+    job->n_splits = prefix_splits;
+    job->row0 = (r - job->split * prefix_blocks) * ROWS;
+    job->n_rows = (t.end - t.first) * G;
+    job->token0 = t.first;
+    job->p0 = 0;
+    job->n_prefix = p.n_prefix;
+    job->own = false;
+    job->table = p.prefix_pages;
+    return job->row0 < job->n_rows;
+}
+template <int ROWS>
+__device__ inline bool find_own_job(const PagedProblem& p, int prefix_blocks, int prefix_splits, int blocks, int splits, int r, int lane, Job* job) {
     const int G = p.n_q_heads / p.n_kv_heads;
     const PagedBatch& b = p.b;
-    if (r < prefix_blocks * prefix_splits) {
-        const TokenRange t = token_range(b);
-        job->split = r / prefix_blocks;
-        job->slot = job->split;
-        job->n_splits = prefix_splits;
-        job->row0 = (r - job->split * prefix_blocks) * ROWS;
-        job->n_rows = (t.end - t.first) * G;
-        job->token0 = t.first;
-        job->p0 = 0;
-        job->n_prefix = p.n_prefix;
-        job->own = false;
-        job->table = p.prefix_pages;
-    } else {
-        r -= prefix_blocks * prefix_splits;
-        job->split = r / blocks;
-        job->slot = job->split + (prefix_blocks > 0 ? prefix_splits : 0);
-        job->n_splits = splits;
-        // A sequence's blocks start at floor(start * G / ROWS) + its number: at least as many as it needs, some stay empty.
-        // The last blocks first: of a long prompt they have the most keys.
-        const int blk = blocks - 1 - (r - job->split * blocks);
-        auto first_block = [&](int i, int start) { return clamped(start, 0, b.n_tokens) * G / ROWS + i; };
-        const int s = find_sequence(b, lane, blk, first_block);
-        const int start = clamped(scalar_word(b.token_start, s), 0, b.n_tokens), end = clamped(scalar_word(b.token_start, s + 1), start, b.n_tokens);
-        job->row0 = (blk - first_block(s, start)) * ROWS;
-        job->n_rows = (end - start) * G;
-        job->token0 = start;
-        job->p0 = clamped(scalar_word(b.kv_len, s), 0, 1 << 30) - (end - start);
-        job->n_prefix = prefix_blocks > 0 ? 0 : p.n_prefix;
-        job->own = true;
-        job->table = b.page_table + s * b.table_stride;
-    }
+    r -= prefix_blocks * prefix_splits;
+    job->split = r / blocks;
+    job->slot = job->split + (prefix_blocks > 0 ? prefix_splits : 0);
+    job->n_splits = splits;
+    // A sequence's blocks start at floor(start * G / ROWS) + its number: at least as many as it needs, some stay empty.
+    // The last blocks first: of a long prompt they have the most keys.
+    const int blk = blocks - 1 - (r - job->split * blocks);
+    auto first_block = [&](int i, int start) { return clamped(start, 0, b.n_tokens) * G / ROWS + i; };
+    const int s = find_sequence(b, lane, blk, first_block);
+    const int start = clamped(scalar_word(b.token_start, s), 0, b.n_tokens), end = clamped(scalar_word(b.token_start, s + 1), start, b.n_tokens);
+    job->row0 = (blk - first_block(s, start)) * ROWS;
+    job->n_rows = (end - start) * G;
+    job->token0 = start;
+    job->p0 = clamped(scalar_word(b.kv_len, s), 0, 1 << 30) - (end - start);
+    job->n_prefix = prefix_blocks > 0 ? 0 : p.n_prefix;
+    job->own = true;
+    job->table = b.page_table + s * b.table_stride;
     return job->row0 >= 0 && job->row0 < job->n_rows;
 }
 
@@ -96,7 +98,7 @@ template <int T>
 struct Tiles {
     int n_prefix_tiles, n_sink_tiles, n;
     int n_prefix, sinks, first, hi, lo;       // own: the window part starts at key `first`; keys some row sees: [0, sinks) and [lo, hi)
-    // tiles that all rows see whole: [0, a), [n_prefix_tiles, b) and [c, d)
+    // tiles that all rows see whole: [0, a) of the prefix, [n_prefix_tiles, b) of the first tokens, [c, d) of the window part
     int a, b, c, d;
 
     __device__ Tiles(const PagedProblem& p, const Job& j, int first_tok, int last_tok) {
@@ -126,7 +128,7 @@ struct Tiles {
         }
         const int own0 = n_prefix_tiles + n_sink_tiles;
         n = own0 + (hi > first ? (hi - first + T - 1) / T : 0);
-        b = n_prefix_tiles + (sinks < hi_all ? sinks : hi_all) / T;
+        b = n_sink_tiles > 0 ? n_prefix_tiles + (sinks < hi_all ? sinks : hi_all) / T : n_prefix_tiles;
         c = own0 + (lo_all > first ? lo_all - first + T - 1 : 0) / T;
         d = own0 + (hi_all > first ? hi_all - first : 0) / T;
     }
@@ -148,16 +150,23 @@ struct Tiles {
         }
         *r1 = end - k0 < T ? end - k0 - 1 : T - 1;
     }
-    // whether tiles [t, t + count) are all seen whole by all rows
-    __device__ bool whole(int t, int count) const {
-        const int end = t + count;
-        return end <= a || (t >= n_prefix_tiles && end <= b) || (t >= c && end <= d);
-    }
+    // whether all rows see tile t whole
+    __device__ bool whole(int t) const { return t < a || (t >= n_prefix_tiles && t < b) || (t >= c && t < d); }
 };
 
-// Whether the token at index p sees own key j.
-__device__ inline bool sees(const PagedProblem& p, int pos, int hi, int j) {
-    return j < hi && (p.window < 0 || pos - j < p.window || j < p.sinks);
+// What a row sees of a part: keys [lo, hi) and those below `first`.
+struct Seen {
+    int lo, hi, first;
+    __device__ bool operator()(int key) const { return (uint32_t)(key - lo) < (uint32_t)(hi - lo) | key < first; }
+};
+// Of the own keys, for the token at index pos.
+__device__ inline Seen seen_by(const PagedProblem& p, int pos) {
+    Seen s = {0, clamped(pos + 1, 0, p.b.capacity), 0};
+    if (p.window >= 0) {
+        s.lo = clamped(pos + 1 - p.window, 0, s.hi);
+        s.first = p.sinks < s.lo ? p.sinks : s.lo;
+    }
+    return s;
 }
 
 }  // namespace rekv
