@@ -12,22 +12,35 @@ __device__ inline int32_t scalar_word(const int32_t* p, int64_t i) {
     return reinterpret_cast<constant_ptr>(reinterpret_cast<uintptr_t>(p))[i];
 }
 
+__device__ inline int clamped(int v, int lo, int hi) { return v < lo ? lo : v < hi ? v : hi; }
+
+struct Sequence {
+    int i, start, end, kv;      // its number, token rows [start, end) and length, within their bounds
+};
+
 // The last sequence i whose off(i, token_start[i]) is at most `target`; off does not decrease, and that of sequence 0 counts as
-// reached.  A wavefront narrows 64 to one at a time.
+// reached.  A wavefront narrows 64 to one at a time, and reads what the last 64 hold with the same round trip.
 template <class Off>
-__device__ inline int find_sequence(const PagedBatch& b, int lane, int target, Off off) {
+__device__ inline Sequence find_sequence(const PagedBatch& b, int lane, int target, Off off) {
     int lo = 0, n = b.n_seqs;
-    while (n > 1) {
+    while (n > 64) {
         const int step = (n + 63) / 64, i = lane * step;
-        const bool reached = i == 0 || (i < n && off(lo + i, b.token_start[lo + i]) <= target);
+        const bool reached = i == 0 || (i < n && off(lo + i, b.token_start[i < n ? lo + i : lo]) <= target);
         const int last = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(reached));
         lo += last * step;
         n = n - last * step < step ? n - last * step : step;
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+    const int j = lane < n ? lo + lane : lo;
+    const int start = b.token_start[j], end = b.token_start[j + 1], kv = b.kv_len[j];
+    const bool reached = lane == 0 || (lane < n && off(j, start) <= target);
+    const int last = 63 - __builtin_clzll(__builtin_amdgcn_ballot_w64(reached));
+    Sequence s;
+    s.i = lo + last;
+    s.start = clamped(__builtin_amdgcn_readlane(start, last), 0, b.n_tokens);
+    s.end = clamped(__builtin_amdgcn_readlane(end, last), s.start, b.n_tokens);
+    s.kv = clamped(__builtin_amdgcn_readlane(kv, last), 0, 1 << 30);
+    return s;
 }
-
-__device__ inline int clamped(int v, int lo, int hi) { return v < lo ? lo : v < hi ? v : hi; }
 
 // The batch's token rows that belong to sequences: [first, end).
 struct TokenRange {
@@ -80,15 +93,14 @@ __device__ inline bool find_own_job(const PagedProblem& p, int prefix_blocks, in
     // The last blocks first: of a long prompt they have the most keys.
     const int blk = blocks - 1 - (r - job->split * blocks);
     auto first_block = [&](int i, int start) { return clamped(start, 0, b.n_tokens) * G / ROWS + i; };
-    const int s = find_sequence(b, lane, blk, first_block);
-    const int start = clamped(scalar_word(b.token_start, s), 0, b.n_tokens), end = clamped(scalar_word(b.token_start, s + 1), start, b.n_tokens);
-    job->row0 = (blk - first_block(s, start)) * ROWS;
-    job->n_rows = (end - start) * G;
-    job->token0 = start;
-    job->p0 = clamped(scalar_word(b.kv_len, s), 0, 1 << 30) - (end - start);
+    const Sequence s = find_sequence(b, lane, blk, first_block);
+    job->row0 = (blk - first_block(s.i, s.start)) * ROWS;
+    job->n_rows = (s.end - s.start) * G;
+    job->token0 = s.start;
+    job->p0 = s.kv - (s.end - s.start);
     job->n_prefix = prefix_blocks > 0 ? 0 : p.n_prefix;
     job->own = true;
-    job->table = b.page_table + s * b.table_stride;
+    job->table = b.page_table + s.i * b.table_stride;
     return job->row0 >= 0 && job->row0 < job->n_rows;
 }
 
