@@ -183,7 +183,7 @@ struct PagedProblem {
 // per row and split where there is more than one in all.
 struct PagedPlan {
     int32_t rows, blocks, splits, prefix_blocks, prefix_splits;
-    int32_t min_tiles;                  // a split has at least so many 32-key tiles
+    int32_t min_tiles, min_prefix_tiles;   // a split of the own keys and of the prefix has at least so many 32-key tiles
     int64_t workspace_bytes;
     int32_t slots() const { return splits + (prefix_blocks > 0 ? prefix_splits : 0); }
 };
