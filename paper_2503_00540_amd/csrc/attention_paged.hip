@@ -641,8 +641,8 @@ __global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(Pa
     const int r = unit / groups, g = unit - r * groups;
     const int64_t n_rows = (int64_t)p.b.n_tokens * p.n_q_heads;
     const int64_t row = (int64_t)blockIdx.x * rows_per_block + r;
-    const TokenRange range = token_range(p.b);
-    const bool ok = r < rows_per_block && row >= (int64_t)range.first * p.n_q_heads && row < (int64_t)range.end * p.n_q_heads;
+    const TokenRange range = token_range(p.b);       // (looked at when the partial results are on their way)
+    bool ok = r < rows_per_block && row < n_rows;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
     if (ok) {
@@ -675,6 +675,7 @@ __global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(Pa
             m = m_new;
         }
     }
+    ok = ok && row >= (int64_t)range.first * p.n_q_heads && row < (int64_t)range.end * p.n_q_heads;
     if (groups > 1) {
         red_o[tid] = acc;
         red_m[tid] = m;
@@ -682,12 +683,13 @@ __global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(Pa
         __syncthreads();
         if (!ok || g != 0) return;
         float m_all = m;
+#pragma unroll 8
         for (int i = 1; i < groups; ++i) m_all = fmaxf(m_all, red_m[tid + i * tpr]);
         const float ref = m_all == -INFINITY ? 0.f : m_all;
         acc = f32x4{0.f, 0.f, 0.f, 0.f};
         l = 0.f;
-        for (int i = 0; i < groups; ++i) {
-            if (red_m[tid + i * tpr] == -INFINITY) continue;
+#pragma unroll 8
+        for (int i = 0; i < groups; ++i) {       // (a group of no keys has the weight 0 and sums of 0)
             const float w = __builtin_amdgcn_exp2f(red_m[tid + i * tpr] - ref);
             acc += red_o[tid + i * tpr] * w;
             l += red_l[tid + i * tpr] * w;

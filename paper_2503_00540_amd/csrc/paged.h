@@ -68,13 +68,13 @@ struct Job {
 // row blocks fastest.  False: no work.
 template <int ROWS>
 __device__ inline bool find_prefix_job(const PagedProblem& p, int prefix_blocks, int prefix_splits, int r, Job* job) {
+    // (rows of no sequence too: the merge leaves them out, and nothing has to be looked up)
     const int G = p.n_q_heads / p.n_kv_heads;
-    const TokenRange t = token_range(p.b);
     job->split = job->slot = r / prefix_blocks;
     job->n_splits = prefix_splits;
     job->row0 = (r - job->split * prefix_blocks) * ROWS;
-    job->n_rows = (t.end - t.first) * G;
-    job->token0 = t.first;
+    job->n_rows = p.b.n_tokens * G;
+    job->token0 = 0;
     job->p0 = 0;
     job->n_prefix = p.n_prefix;
     job->own = false;
