@@ -389,10 +389,11 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
     int t_begin, t_end;
     split_range(a, job, tiles.n, &t_begin, &t_end);
     const Src src(p, job, tiles, t_end, kvh, lane, wave);
+    Places places;
+    if (t_begin < t_end) src.fill(places, t_begin);      // (before the queries' loads, whose wait this one would be otherwise)
     const Operands<D> at(lds0, lds0 + VB, lane);
     Rows<D> r(p, job, job.row0 + wave * WM + (lane & 31), kvh, G, hh);
 
-    Places places;
     Place at_k, at_v;                        // of tiles t + 4 and t + 3 in step t
     uint32_t whole = 0;                      // bit i: all rows see tile t + i whole
     auto fetch = [&](int t, uint32_t kl, uint32_t vl) __attribute__((always_inline)) {      // the loads of step t
@@ -434,7 +435,6 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
     if (t_begin < t_end) {
         if (tid == 0) *sh_dropped = 0;       // before the first barrier
         f32x16 s_a, s_b;
-        src.fill(places, t_begin);
 #pragma unroll 1
         for (int i = 0; i < 4; ++i) {        // K of four tiles, V of three
             const int t = src.in_list(t_begin + i);
