@@ -23,6 +23,7 @@ constexpr int THREADS = WAVES * 64;
 constexpr int WM = 32;                // rows of a wavefront
 constexpr int BM = WAVES * WM;        // rows of a block whose wavefronts share the tiles
 constexpr int STAGES = 4;             // of such a block, per tensor
+enum { ROW_BLOCKS, KEY_BLOCKS, STREAMED };
 
 struct PagedArgs {
     PagedProblem p;
@@ -499,10 +500,11 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
 }
 
 // A block of 32 rows, as a decode step's: its four wavefronts divide the KEYS, each walks its run of tiles through a K and a V tile
-// of its own in LDS without a barrier, and their results meet in LDS.  Nobody else reads the keys, so loads are non-temporal.
-template <int D, bool TWO_PAGES>
+// of its own in LDS without a barrier, and their results meet in LDS.  STREAM: non-temporal loads, where nobody else reads the keys (64 users'
+// decode step 201 us so, 224 with cached loads).
+template <int D, bool TWO_PAGES, bool STREAM>
 __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, const Job& job, int kvh, unsigned char* lds, f32x2 (*ml)[WM]) {
-    typedef Source<D, TWO_PAGES, 1, true> Src;
+    typedef Source<D, TWO_PAGES, 1, STREAM> Src;
     constexpr uint32_t TILE_B = Src::TILE_B;
     constexpr int N_DMA = Src::N_DMA, CPR = D / 4;       // 16-byte fp32 chunks per output row
     const PagedProblem& p = a.p;
@@ -607,10 +609,11 @@ __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, co
     }
 }
 
-// FEW: the sequences' own keys by blocks of 32 rows, a prefix shared by the batch still by blocks of 128 (a batch of 42 rows over 3,136
+// ROW_BLOCKS: all by blocks of 128 rows.  KEY_BLOCKS, STREAMED: the sequences' own keys by blocks of 32 rows, a prefix shared by the batch still by blocks of 128 (a batch of 42 rows over 3,136
 // prefix tokens takes 11.1 us so, 10.8 to 11.6 by blocks of 32).
-template <int D, bool TWO_PAGES, bool FEW>
+template <int D, bool TWO_PAGES, int HOW>
 __global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
+    constexpr bool FEW = HOW != ROW_BLOCKS;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * STAGES * BN * D * 2];
     __shared__ f32x2 ml[FEW ? WAVES : 1][WM];
     __shared__ int sh_dropped;
@@ -619,7 +622,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
     const bool prefix = L < a.prefix_blocks * a.prefix_splits;
     Job job;
     if (FEW && !prefix) {
-        if (find_own_job<WM>(a.p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)) keys_block<D, TWO_PAGES>(a, job, kvh, lds, ml);
+        if (find_own_job<WM>(a.p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)) keys_block<D, TWO_PAGES, HOW == STREAMED>(a, job, kvh, lds, ml);
         return;
     }
     if (prefix ? find_prefix_job<BM>(a.p, a.prefix_blocks, a.prefix_splits, L, &job)
@@ -1023,6 +1026,7 @@ __global__ __launch_bounds__(VECTOR_ROWS * 64) void attn_paged_f32_kernel(PagedA
 }
 
 int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
+constexpr int64_t PLACES = 512;       // workgroups of a bf16 launch that the chip holds: two per CU
 
 }  // namespace
 
@@ -1031,14 +1035,24 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     const int64_t G = n_q_heads / n_kv_heads, all_rows = n_tokens * G;
     const bool bf16 = dtype == REKV_BF16;
     PagedPlan plan;
-    const bool few = bf16 && all_rows <= n_seqs * WM;
+    int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
+    // Blocks of 32 rows start and end sooner but fetch every tile four times as often: they take the sequences' own keys where few rows of
+    // a sequence share them, and where there is little to do in all: up to SMALL tiles of 128 rows per place.  28/4/128 and 14/2/64, as
+    // blocks of 128 and of 32 rows (us): a prompt of 196 tokens 13.8 and 8.6, 16 tokens over 3,000 17.8 and 14.1, a prompt of 1,000 34.7
+    // and 28.5, a live frame over 3,136 at 14/2/64 22.1 and 16.8; the other way 4 x 8 tokens over 8,000 18.7 and 20.4 (7.8 tiles a place),
+    // 32 x 16 over 3,000 42 and 58 (23), 4 live frames of 64/8/128 53 and 64 (23).
+    constexpr int64_t SMALL = 6;
+    const int64_t row_blocks = up(all_rows, BM) > n_seqs ? up(all_rows, BM) : n_seqs;
+    const bool lone = all_rows <= n_seqs * WM;
+    const bool few = bf16 && (lone || row_blocks * n_kv_heads * up(keys + n_prefix, BN) <= SMALL * PLACES);
+    plan.how = !few ? ROW_BLOCKS : lone ? STREAMED : KEY_BLOCKS;
     plan.rows = !bf16 ? head_dim == 64 || head_dim == 128 ? F32_ROWS : VECTOR_ROWS : few ? WM : BM;
     const int64_t prefix_rows = bf16 ? BM : plan.rows;
     plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
     // (two tiles a wavefront: a user's window of 15,000 tokens at 28/4/128 takes 16.7 us so, 18.7 with one, 17.5 with three)
     plan.min_tiles = few ? 8 : 4;
     plan.min_prefix_tiles = 4;
-    const int64_t places = bf16 ? 512 : 1024;
+    const int64_t places = bf16 ? PLACES : 1024;
     // The splits that fill `places` workgroups with `busy` ones, of at least `least` and about at most `most` tiles.
     auto splits_of = [&](int64_t places, int64_t busy, int64_t tiles, int64_t least, int64_t most) {
         int64_t s = places / (busy * n_kv_heads);
@@ -1047,7 +1061,6 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
         return (int32_t)(s < 1 ? 1 : s);
     };
     plan.prefix_blocks = plan.prefix_splits = 0;
-    int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
     const int64_t busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
     // Rows that fill blocks by themselves walk the prefix in their own blocks.
     const bool together = n_prefix > 0 && all_rows < n_seqs * (prefix_rows / 2);
@@ -1066,12 +1079,11 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     return plan;
 }
 
-template <int D>
-void launch_bf16(const PagedArgs& a, bool two_pages, bool few, dim3 grid, hipStream_t stream) {
-    if (two_pages && few) hipLaunchKernelGGL((attn_paged_kernel<D, true, true>), grid, dim3(THREADS), 0, stream, a);
-    else if (two_pages) hipLaunchKernelGGL((attn_paged_kernel<D, true, false>), grid, dim3(THREADS), 0, stream, a);
-    else if (few) hipLaunchKernelGGL((attn_paged_kernel<D, false, true>), grid, dim3(THREADS), 0, stream, a);
-    else hipLaunchKernelGGL((attn_paged_kernel<D, false, false>), grid, dim3(THREADS), 0, stream, a);
+template <int D, bool TWO_PAGES>
+void launch_bf16(const PagedArgs& a, int how, dim3 grid, hipStream_t stream) {
+    if (how == STREAMED) hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, STREAMED>), grid, dim3(THREADS), 0, stream, a);
+    else if (how == KEY_BLOCKS) hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, KEY_BLOCKS>), grid, dim3(THREADS), 0, stream, a);
+    else hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, ROW_BLOCKS>), grid, dim3(THREADS), 0, stream, a);
 }
 
 hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int dtype, void* workspace, hipStream_t stream) {
@@ -1089,8 +1101,8 @@ hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int d
     if (dtype == REKV_F32 && p.head_dim == 64) hipLaunchKernelGGL(attn_paged_f32_mfma_kernel<64>, grid, dim3(THREADS), 0, stream, a);
     else if (dtype == REKV_F32 && p.head_dim == 128) hipLaunchKernelGGL(attn_paged_f32_mfma_kernel<128>, grid, dim3(THREADS), 0, stream, a);
     else if (dtype == REKV_F32) hipLaunchKernelGGL(attn_paged_f32_kernel, grid, dim3(VECTOR_ROWS * 64), 0, stream, a);
-    else if (p.head_dim == 128) launch_bf16<128>(a, two_pages, plan.rows == WM, grid, stream);
-    else launch_bf16<64>(a, two_pages, plan.rows == WM, grid, stream);
+    else if (p.head_dim == 128) (two_pages ? launch_bf16<128, true> : launch_bf16<128, false>)(a, plan.how, grid, stream);
+    else (two_pages ? launch_bf16<64, true> : launch_bf16<64, false>)(a, plan.how, grid, stream);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_slots == 1) return e;
     const int tpr = p.head_dim / 4, threads = a.n_slots > 32 ? MOST_MERGE_THREADS : 256, units = threads / tpr;

@@ -182,6 +182,7 @@ struct PagedProblem {
 // for the whole batch at once (prefix_blocks > 0), for the prefix; splits of the keys of either; a partial result
 // per row and split where there is more than one in all.
 struct PagedPlan {
+    int32_t how;                        // bf16: the kernel's form
     int32_t rows, blocks, splits, prefix_blocks, prefix_splits;
     int32_t min_tiles, min_prefix_tiles;   // a split of the own keys and of the prefix has at least so many 32-key tiles
     int64_t workspace_bytes;
