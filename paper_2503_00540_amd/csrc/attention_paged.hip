@@ -128,12 +128,6 @@ struct Source {
         }
         return at;
     }
-    // Row r of a tile in two pages: lanes of either take a load of their own, from a uniform address.  Where a load has lanes
-    // of both, one more is in flight than is counted below, which only makes a wait longer.
-    __device__ __attribute__((always_inline)) void fetch_row(const char* base, const Place& at, int r, uint32_t o, uint32_t dst) const {
-        if (r < at.rows_a) dma16<STREAM>(base + at.a * (int64_t)row_b, o, dst);
-        else dma16<STREAM>(base + at.b * (int64_t)row_b, o, dst);
-    }
     // This wavefront's share of a tile.  Rows that no row of the block sees repeat the nearest that one does.
     __device__ __attribute__((always_inline)) void fetch(const char* base, int t, const Place& at, uint32_t dst) const {
         dst += (uint32_t)(loader * N_DMA) * 1024u;
@@ -143,26 +137,38 @@ struct Source {
                 const int r = first_row + j * RPI, row = __shfl(at.a, LOADERS > 1 ? r & 7 : r);
                 dma16_at(reinterpret_cast<uint64_t>(base) + (uint64_t)(uint32_t)row * row_b + chunk(r), dst + j * 1024u);
             }
-        } else if (at.whole && at.rows_a >= BN) {
+            return;
+        }
+        const char* in_a = base + (int64_t)at.a * row_b;
+        if (at.whole && at.rows_a >= BN) {
 #pragma unroll
-            for (int j = 0; j < N_DMA; ++j)
-                dma16<STREAM>(base + (int64_t)(at.a + j / N_OFF * 16) * row_b, off[j % N_OFF], dst + j * 1024u);
-        } else {
-            int r0 = 0, r1 = BN - 1;
-            if (!at.whole) tiles.rows(t, &r0, &r1);
-            if (N_DMA <= 2) {
+            for (int j = 0; j < N_DMA; ++j) dma16<STREAM>(in_a + (uint32_t)(j / N_OFF * 16) * row_b, off[j % N_OFF], dst + j * 1024u);
+            return;
+        }
+        // Lanes of either page take a load of their own, from a uniform address.  Where a load has lanes of both, one more is in
+        // flight than is counted, which only makes a wait longer.
+        const char* in_b = base + (int64_t)at.b * row_b;
+        auto row_of = [&](int r, uint32_t o, uint32_t to) __attribute__((always_inline)) {
+            if (r < at.rows_a) dma16<STREAM>(in_a, o, to);
+            else dma16<STREAM>(in_b, o, to);
+        };
+        if (at.whole) {
 #pragma unroll
-                for (int j = 0; j < N_DMA; ++j) {
-                    const int r = clamped(first_row + j * RPI, r0, r1);
-                    fetch_row(base, at, r, (uint32_t)r * row_b + chunk(first_row + j * RPI), dst + j * 1024u);
-                }
-            } else {
-#pragma unroll 1
-                for (int j = 0; j < N_DMA; ++j) {
-                    const int r = clamped(first_row + j * RPI, r0, r1);
-                    fetch_row(base, at, r, (uint32_t)r * row_b + chunk(first_row + j * RPI), dst + j * 1024u);
-                }
+            for (int j = 0; j < N_DMA; ++j) {
+                const int first = (loader * N_DMA + j) * RPI;                      // of the load's rows
+                const uint32_t on = (uint32_t)(j / N_OFF * 16) * row_b, to = dst + j * 1024u;
+                if (first + RPI <= at.rows_a) dma16<STREAM>(in_a + on, off[j % N_OFF], to);
+                else if (first >= at.rows_a) dma16<STREAM>(in_b + on, off[j % N_OFF], to);
+                else row_of(first_row + j * RPI, off[j % N_OFF] + on, to);
             }
+            return;
+        }
+        int r0, r1;
+        tiles.rows(t, &r0, &r1);
+#pragma unroll 1
+        for (int j = 0; j < N_DMA; ++j) {
+            const int r = clamped(first_row + j * RPI, r0, r1);
+            row_of(r, (uint32_t)r * row_b + chunk(first_row + j * RPI), dst + j * 1024u);
         }
     }
 };
@@ -710,8 +716,8 @@ __global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(Pa
     }
 }
 
-// ---- fp32, head_dim 64 and 128: true fp32 products and sums on the matrix cores, operands straight from memory as in
-// attention_f32.hip.  A workgroup's four wavefronts share 16 stacked rows and take the 32-key tiles in turn; their (maximum, sum, O)
+// ---- fp32: true fp32 products and sums on the matrix cores, operands straight from memory as in attention_f32.hip.  Head sizes between
+// 64, 128 and 256 (D_MAX) are padded with zeros in the registers.  A workgroup's four wavefronts share 16 stacked rows and take the 32-key tiles in turn; their (maximum, sum, O)
 // meet in LDS.  Bound, at the sizes that fp32 serves, by the round trips to the first key.  The tiny configuration's ragged batch
 // (5 sequences, window 77) takes 8.1 us, on the vector ALU below 21.5.
 constexpr int F32_ROWS = 16;
@@ -729,10 +735,12 @@ __device__ inline float quad_combine(float v) {
     return op(t[0], t[1]);
 }
 
-template <int D>
-__global__ __launch_bounds__(THREADS, 2) void attn_paged_f32_mfma_kernel(PagedArgs a) {
-    constexpr int QD = D / 4;                     // dims per lane of a Q or K row
-    constexpr int VB = D / 64;                    // 64-dim blocks of V and O
+template <int D_MAX, bool PADDED>
+__global__ __launch_bounds__(THREADS, D_MAX > 128 ? 1 : 2) void attn_paged_f32_kernel(PagedArgs a) {
+    constexpr int QD = D_MAX / 4;                 // dims per lane of a Q or K row
+    constexpr int VB = D_MAX / 64;                // 64-dim blocks of V and O
+    const int D = PADDED ? a.p.head_dim : D_MAX;
+    auto load4 = [&](const float* v, int dim) { return !PADDED || dim < D ? *reinterpret_cast<const f32x4*>(v + dim) : f32x4{0.f, 0.f, 0.f, 0.f}; };
     __shared__ f32x4 o_lds[WAVES][VB * 4][64];
     __shared__ float m_lds[WAVES][F32_ROWS], l_lds[WAVES][F32_ROWS];
     const PagedProblem& p = a.p;
@@ -763,7 +771,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_f32_mfma_kernel(PagedAr
     const float* qp = static_cast<const float*>(p.q) + q_row * D;
     f32x4 qf[QD / 4];
 #pragma unroll
-    for (int i = 0; i < QD / 4; ++i) qf[i] = row_ok ? *reinterpret_cast<const f32x4*>(qp + g * QD + i * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < QD / 4; ++i) qf[i] = row_ok ? load4(qp, g * QD + i * 4) : f32x4{0.f, 0.f, 0.f, 0.f};
     f32x4 o[VB][4];
 #pragma unroll
     for (int b = 0; b < VB; ++b)
@@ -778,17 +786,17 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_f32_mfma_kernel(PagedAr
         f32x4 kf[2][QD / 4], vf[2][4][VB];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const float* k = static_cast<const float*>(p.b.k_pages) + of_lane(at, kb * 16 + r) * D + g * QD;
+            const float* k = static_cast<const float*>(p.b.k_pages) + of_lane(at, kb * 16 + r) * D;
 #pragma unroll
-            for (int i = 0; i < QD / 4; ++i) kf[kb][i] = *reinterpret_cast<const f32x4*>(k + i * 4);
+            for (int i = 0; i < QD / 4; ++i) kf[kb][i] = load4(k, g * QD + i * 4);
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj) {
-                const float* v = static_cast<const float*>(p.b.v_pages) + of_lane(at, kb * 16 + g * 4 + jj) * D + r * 4;
+                const float* v = static_cast<const float*>(p.b.v_pages) + of_lane(at, kb * 16 + g * 4 + jj) * D;
 #pragma unroll
-                for (int b = 0; b < VB; ++b) vf[kb][jj][b] = *reinterpret_cast<const f32x4*>(v + b * 64);
+                for (int b = 0; b < VB; ++b) vf[kb][jj][b] = load4(v, b * 64 + r * 4);
             }
         if (t + WAVES < t_end) next = places(t + WAVES);
         __builtin_amdgcn_sched_barrier(0);       // the loads leave together
@@ -873,7 +881,7 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_f32_mfma_kernel(PagedAr
                 if (!sees(key)) continue;
                 const int slot = (int)quot((uint32_t)key, p.b.by_page);
                 const int64_t at = (((int64_t)clamped(table[slot], 0, p.b.n_pages - 1) * page + (key - slot * page)) * p.n_kv_heads + kvh) * D;
-                const float *kr = static_cast<const float*>(p.b.k_pages) + at, *vr = static_cast<const float*>(p.b.v_pages) + at + g * 16;
+                const float *kr = static_cast<const float*>(p.b.k_pages) + at, *vr = static_cast<const float*>(p.b.v_pages) + at;
                 float s = 0.f;
 #pragma unroll 1
                 for (int d = 0; d < D; ++d) s = fmaf(kr[d], qp[d], s);
@@ -881,12 +889,11 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_f32_mfma_kernel(PagedAr
 #pragma unroll
                 for (int b = 0; b < VB; ++b)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < 4; ++i) {
+                        const f32x4 v = load4(vr, b * 64 + g * 16 + i * 4);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float v = vr[b * 64 + i * 4 + e];
-                            o[b][e][i] = fmaf(pj, __builtin_fabsf(v) < INFINITY ? 0.f : v, o[b][e][i]);
-                        }
+                        for (int e = 0; e < 4; ++e) o[b][e][i] = fmaf(pj, __builtin_fabsf(v[e]) < INFINITY ? 0.f : v[e], o[b][e][i]);
+                    }
             }
         }
     }
@@ -911,118 +918,17 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_f32_mfma_kernel(PagedAr
     }
     const int64_t to = (int64_t)job.slot * p.b.n_tokens * p.n_q_heads + q_row;
     const float inv = a.n_slots > 1 ? 1.f : l_all == 0.f ? 0.f : 1.f / l_all;
-    float* out = (a.n_slots > 1 ? a.part_o + to * D : static_cast<float*>(p.out) + q_row * D) + g * 16;
+    float* out = (a.n_slots > 1 ? a.part_o + to * D : static_cast<float*>(p.out) + q_row * D);
     for (int c = wave; c < VB * 4; c += WAVES) {          // a wavefront each four dims of a 64-dim block
+        const int dim = c / 4 * 64 + g * 16 + c % 4 * 4;
+        if (PADDED && dim >= D) continue;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < WAVES; ++i)
             if (w[i] != 0.f) v += o_lds[i][c][lane] * w[i];
-        *reinterpret_cast<f32x4*>(out + c / 4 * 64 + c % 4 * 4) = v * inv;
+        *reinterpret_cast<f32x4*>(out + dim) = v * inv;
     }
     if (a.n_slots > 1 && wave == 0 && g == 0) *reinterpret_cast<f32x2*>(a.part_ml + to * 2) = f32x2{m_all, l_all};
-}
-
-// Other head sizes: plain vector-ALU code, one wavefront per row.  The keys a row sees are numbered through, first tokens, then window (or the
-// prefix), and a split takes a run of them; 64 keys at a time each lane scores one, then the lanes own output dimensions.
-constexpr int VECTOR_ROWS = 4;
-constexpr int MAX_D = 256;
-__device__ inline float wave_max(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ inline float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
-__global__ __launch_bounds__(VECTOR_ROWS * 64) void attn_paged_f32_kernel(PagedArgs a) {
-    __shared__ float q_lds[VECTOR_ROWS][MAX_D];
-    __shared__ float p_lds[VECTOR_ROWS][64];
-    __shared__ int64_t at_lds[VECTOR_ROWS][64];
-    const PagedProblem& p = a.p;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int D = p.head_dim, G = p.n_q_heads / p.n_kv_heads;
-    const int L = blockIdx.x / p.n_kv_heads, kvh = blockIdx.x - L * p.n_kv_heads;
-    Job job;
-    if (!(L < a.prefix_blocks * a.prefix_splits ? find_prefix_job<VECTOR_ROWS>(p, a.prefix_blocks, a.prefix_splits, L, &job)
-                                                : find_own_job<VECTOR_ROWS>(p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)))
-        return;
-    const int row = job.row0 + wave;
-    if (row >= job.n_rows) return;           // whole wavefront leaves; nothing below waits for the workgroup
-    const int tok = row / G, pos = job.p0 + tok;
-    const int64_t q_row = (int64_t)(job.token0 + tok) * p.n_q_heads + kvh * G + (row - tok * G);
-    const float* q = static_cast<const float*>(p.q) + q_row * D;
-    for (int d = lane; d < D; d += 64) q_lds[wave][d] = q[d];
-    __builtin_amdgcn_wave_barrier();
-
-    // key i of the row's list: prefix, first tokens, window
-    int hi = 0, lo = 0, n_first = 0;
-    if (job.own) {
-        hi = clamped(pos + 1, 0, p.b.capacity);
-        if (p.window >= 0) {
-            lo = clamped(pos + 1 - p.window, 0, hi);
-            n_first = p.sinks < lo ? p.sinks : lo;
-        }
-    }
-    const int n_keys = job.n_prefix + n_first + (hi - lo);
-    int per_split = (n_keys + job.n_splits - 1) / job.n_splits;
-    per_split = per_split > a.min_tiles * BN ? per_split : a.min_tiles * BN;
-    const int begin = job.split * per_split, end = begin + per_split < n_keys ? begin + per_split : n_keys;
-
-    const int page = (int)p.b.by_page.d;
-    float o[MAX_D / 64] = {0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    const float sc = p.scale * 1.4426950408889634f;
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        int j = j0 + lane;
-        float s = -INFINITY;
-        if (j < end) {
-            const bool pre = j < job.n_prefix;
-            const int32_t* table = pre ? p.prefix_pages : job.table;
-            if (!pre) {
-                j -= job.n_prefix;
-                if (j >= n_first) j += lo - n_first;
-            }
-            const int slot = (int)quot((uint32_t)j, p.b.by_page);
-            const int64_t at = (((int64_t)clamped(table[slot], 0, p.b.n_pages - 1) * page + (j - slot * page)) * p.n_kv_heads + kvh) * D;
-            at_lds[wave][lane] = at;
-            const float* k = static_cast<const float*>(p.b.k_pages) + at;
-            float acc = 0.f;
-            for (int d = 0; d < D; d += 4) {
-                const f32x4 x = *reinterpret_cast<const f32x4*>(k + d);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc = fmaf(x[i], q_lds[wave][d + i], acc);
-            }
-            s = acc * sc;
-        }
-        const float m_new = fmaxf(m, wave_max(s)), ref = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m - ref);
-        const float e = j0 + lane < end ? __builtin_amdgcn_exp2f(s - ref) : 0.f;
-        l = l * alpha + wave_sum(e);
-        m = m_new;
-        p_lds[wave][lane] = e;
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int i = 0; i < MAX_D / 64; ++i) o[i] *= alpha;
-        const int n = end - j0 < 64 ? end - j0 : 64;
-        for (int jj = 0; jj < n; ++jj) {
-            const float* v = static_cast<const float*>(p.b.v_pages) + at_lds[wave][jj];
-            const float e_j = p_lds[wave][jj];
-#pragma unroll
-            for (int i = 0; i < MAX_D / 64; ++i)
-                if (lane + 64 * i < D) o[i] = fmaf(e_j, v[lane + 64 * i], o[i]);
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
-    const int64_t at = (int64_t)job.slot * p.b.n_tokens * p.n_q_heads + q_row;
-    const float inv = a.n_slots > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-    float* out = a.n_slots > 1 ? a.part_o + at * D : static_cast<float*>(p.out) + q_row * D;
-#pragma unroll
-    for (int i = 0; i < MAX_D / 64; ++i)
-        if (lane + 64 * i < D) out[lane + 64 * i] = o[i] * inv;
-    if (a.n_slots > 1 && lane == 0) *reinterpret_cast<f32x2*>(a.part_ml + at * 2) = f32x2{l != 0.f ? m : -INFINITY, l};
 }
 
 int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
@@ -1046,7 +952,7 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     const bool lone = all_rows <= n_seqs * WM;
     const bool few = bf16 && (lone || row_blocks * n_kv_heads * up(keys + n_prefix, BN) <= SMALL * PLACES);
     plan.how = !few ? ROW_BLOCKS : lone ? STREAMED : KEY_BLOCKS;
-    plan.rows = !bf16 ? head_dim == 64 || head_dim == 128 ? F32_ROWS : VECTOR_ROWS : few ? WM : BM;
+    plan.rows = !bf16 ? F32_ROWS : few ? WM : BM;
     const int64_t prefix_rows = bf16 ? BM : plan.rows;
     plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
     // (two tiles a wavefront: a user's window of 15,000 tokens at 28/4/128 takes 16.7 us so, 18.7 with one, 17.5 with three)
@@ -1098,9 +1004,15 @@ hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int d
     const int64_t jobs = (int64_t)plan.prefix_blocks * plan.prefix_splits + (int64_t)plan.blocks * plan.splits;
     const dim3 grid((unsigned)(jobs * p.n_kv_heads));
     const bool two_pages = p.b.by_page.d >= BN || p.b.by_page.d == 16;
-    if (dtype == REKV_F32 && p.head_dim == 64) hipLaunchKernelGGL(attn_paged_f32_mfma_kernel<64>, grid, dim3(THREADS), 0, stream, a);
-    else if (dtype == REKV_F32 && p.head_dim == 128) hipLaunchKernelGGL(attn_paged_f32_mfma_kernel<128>, grid, dim3(THREADS), 0, stream, a);
-    else if (dtype == REKV_F32) hipLaunchKernelGGL(attn_paged_f32_kernel, grid, dim3(VECTOR_ROWS * 64), 0, stream, a);
+    if (dtype == REKV_F32) {
+        const int d = p.head_dim;
+        hipLaunchKernelGGL((d == 64    ? attn_paged_f32_kernel<64, false>
+                            : d == 128 ? attn_paged_f32_kernel<128, false>
+                            : d < 64   ? attn_paged_f32_kernel<64, true>
+                            : d < 128  ? attn_paged_f32_kernel<128, true>
+                                       : attn_paged_f32_kernel<256, true>),
+                           grid, dim3(THREADS), 0, stream, a);
+    }
     else if (p.head_dim == 128) (two_pages ? launch_bf16<128, true> : launch_bf16<128, false>)(a, plan.how, grid, stream);
     else (two_pages ? launch_bf16<64, true> : launch_bf16<64, false>)(a, plan.how, grid, stream);
     hipError_t e = hipGetLastError();

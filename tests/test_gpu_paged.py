@@ -8,7 +8,8 @@ from paper_2503_00540_amd.rekv import Rekv
 
 pytestmark = pytest.mark.gpu
 
-HEADS = [(14, 2, 64, "bf16"), (28, 4, 128, "bf16"), (8, 8, 64, "bf16"), (4, 1, 64, "f32"), (6, 2, 20, "f32"), (8, 2, 128, "f32")]
+HEADS = [(14, 2, 64, "bf16"), (28, 4, 128, "bf16"), (8, 8, 64, "bf16"), (4, 1, 64, "f32"), (6, 2, 20, "f32"), (8, 2, 128, "f32"),
+         (6, 2, 80, "f32"), (2, 1, 256, "f32")]
 
 
 def attend(b, window=None, sinks=0, max_kv=None, r=None):
