@@ -411,6 +411,7 @@ typedef struct {
  * D / 2.  order 0: section after section; 1: the pairs go in turn to the axes that have
  * pairs left (time, height, width, time, ...).  layout 0: pair i is (i, i + D / 2), 1: (2i, 2i + 1).
  * inverse 1 turns back, which is also the gradient of a rotation.  Angles are formed in double precision.
+ * rekv_rotate and rekv_append_kv take head_dim a multiple of 16 (bf16) or 8 (fp32).
  */
 typedef struct {
     double base;         /* 1 < base < 1e30 */
@@ -438,7 +439,8 @@ rekv_status rekv_rotate(rekv_ctx* ctx, const rekv_rotary* rotary, const void* x,
  *   positions  device int32 [n_axes, n_tokens]; NULL: a token's position is its index in its
  *              sequence, on every axis
  * kv_len counts the new tokens.  Tokens whose index lies outside the table's max_pages, or whose page
- * is outside [0, n_pages), are not written.  Rows of q_out behind the last sequence stay as they were.
+ * is outside [0, n_pages), are not written; no two tokens may have the same place.  Rows of q_out behind the last
+ * sequence stay as they were.
  */
 rekv_status rekv_append_kv(rekv_ctx* ctx, const rekv_paged* cache, const rekv_rotary* rotary, const void* k,
                            int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,

@@ -955,32 +955,34 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     plan.rows = !bf16 ? F32_ROWS : few ? WM : BM;
     const int64_t prefix_rows = bf16 ? BM : plan.rows;
     plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
-    // (two tiles a wavefront: a user's window of 15,000 tokens at 28/4/128 takes 16.7 us so, 18.7 with one, 17.5 with three)
-    plan.min_tiles = few ? 8 : 4;
-    plan.min_prefix_tiles = 4;
-    const int64_t places = bf16 ? PLACES : 1024;
-    // The splits that fill `places` workgroups with `busy` ones, of at least `least` and about at most `most` tiles.
-    auto splits_of = [&](int64_t places, int64_t busy, int64_t tiles, int64_t least, int64_t most) {
-        int64_t s = places / (busy * n_kv_heads);
-        if (s < tiles / most) s = tiles / most;
-        if (s > tiles / least) s = tiles / least;
-        return (int32_t)(s < 1 ? 1 : s);
-    };
-    plan.prefix_blocks = plan.prefix_splits = 0;
-    const int64_t busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
+    const int64_t places = bf16 ? PLACES : 1024, busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
     // Rows that fill blocks by themselves walk the prefix in their own blocks.
     const bool together = n_prefix > 0 && all_rows < n_seqs * (prefix_rows / 2);
-    if (together) {
-        // (beside the own keys' workgroups, which are short: half a place each)
-        const int64_t free_places = places - busy * n_kv_heads / 2;
-        plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
-        plan.prefix_splits = splits_of(free_places > places / 4 ? free_places : places / 4, plan.prefix_blocks, up(n_prefix, BN), plan.min_prefix_tiles,
-                                       1 << 30);
-    } else {
-        keys += n_prefix;
+    const int64_t tiles = up(together ? keys : keys + n_prefix, BN);
+    // As many splits as fill the chip, each of two tiles a wavefront at least (a user's window of 15,000 tokens at 28/4/128 takes 16.7 us so,
+    // 18.7 with one, 17.5 with three).
+    plan.min_tiles = few ? 8 : 4;
+    int64_t s = places / (busy * n_kv_heads);
+    if (s > tiles / plan.min_tiles) s = tiles / plan.min_tiles;
+    // Where lone rows all but fill it, their lengths differ: pieces of one size, LONG tiles, spread the longer ones (64 users of 1 to 8,192
+    // tokens at 64/8/128: 221 us whole, 207, 199, 199, 205 in pieces of 96, 64, 48, 32).
+    constexpr int64_t LONG = 64, MOST_PIECES = 64;
+    if (few && s < 8 && s < tiles / LONG && busy * n_kv_heads < 4 * PLACES) {
+        s = tiles / LONG < MOST_PIECES ? tiles / LONG : MOST_PIECES;
+        plan.min_tiles = (int32_t)LONG;
     }
-    plan.splits = splits_of(places, busy, up(keys, BN), plan.min_tiles, few ? 64 : 1 << 30);
-    if (plan.splits > 1) plan.min_tiles = (int32_t)up(up(keys, BN), plan.splits);
+    plan.splits = (int32_t)(s < 1 ? 1 : s);
+    plan.prefix_blocks = plan.prefix_splits = 0;
+    plan.min_prefix_tiles = 4;
+    if (together) {
+        // beside the own keys' workgroups, which are short: half a place each (64 users over 25,088 tokens at 28/4/128, us: 48.5 with 24 splits, as
+        // this gives, 56.0 with 32, 50.6 with 16)
+        const int64_t left = places - busy * n_kv_heads / 2, prefix_tiles = up(n_prefix, BN);
+        plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
+        int64_t n = (left > places / 4 ? left : places / 4) / (plan.prefix_blocks * n_kv_heads);
+        if (n > prefix_tiles / plan.min_prefix_tiles) n = prefix_tiles / plan.min_prefix_tiles;
+        plan.prefix_splits = (int32_t)(n < 1 ? 1 : n);
+    }
     plan.workspace_bytes = plan.slots() > 1 ? n_tokens * n_q_heads * plan.slots() * (head_dim + 2) * 4 : 0;
     return plan;
 }

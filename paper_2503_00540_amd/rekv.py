@@ -565,8 +565,8 @@ class Rekv:
 
     def _rotary(self, sections, base, layout, order, inverse=False):
         sections = [self.head_dim // 2] if sections is None else list(sections)
-        if not 1 <= len(sections) <= 4:
-            raise ValueError("sections must name 1 to 4 axes")
+        if not 1 <= len(sections) <= 4 or not all(0 <= n <= self.head_dim for n in sections):
+            raise ValueError(f"sections={sections} must name the pairs of 1 to 4 axes")
         return RekvRotary(base, {"half": 0, "interleaved": 1}[layout], {"blocks": 0, "turns": 1}[order], int(inverse), len(sections),
                           (c_int32 * 4)(*sections))
 
@@ -629,7 +629,9 @@ class Rekv:
         if v.shape[0] != n:
             raise ValueError("k and v must hold as many tokens")
         rotary = self._rotary(sections, base, layout, order) if rotate else None
-        p_stride = 0 if positions is None or rotary is None else self._positions(positions, n, rotary.n_axes)
+        if positions is not None and rotary is None:
+            raise ValueError("positions without a rotation")
+        p_stride = 0 if positions is None else self._positions(positions, n, rotary.n_axes)
         self._check(self._lib.rekv_append_kv(
             self._h, byref(cache), byref(rotary) if rotate else None, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
             q.data_ptr() if q is not None else None, q_stride, q_out.data_ptr() if q is not None else None,
@@ -640,7 +642,8 @@ class Rekv:
         qh = (self.n_q_heads, self.head_dim)
         if q.dim() != 3:
             raise ValueError("q must be [n_tokens, Hq, D]")
-        max_kv = cache.max_pages * cache.page_size if max_kv is None else max_kv
+        # (c_int32 would wrap; beyond 2^30 a window is none, and sinks and max_kv mean the same)
+        max_kv, window, sinks = (min(x, (1 << 31) - 1) for x in (cache.max_pages * cache.page_size if max_kv is None else max(max_kv, 0), window, sinks))
         out = torch.empty_like(q) if out is None else out
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
@@ -668,6 +671,8 @@ class Rekv:
         self._here(q=q, out=out)
         if window is not None and window < 0:
             raise ValueError(f"window={window} must not be negative (None: no window)")
+        if sinks < 0:
+            raise ValueError(f"sinks={sinks} must not be negative")
         cache = self._paged(k_pages, v_pages, token_start, kv_len, page_table, q.shape[0])
         return self._attention_paged(q, cache, 0, None, max_kv, -1 if window is None else window, sinks, out)
 
@@ -682,7 +687,7 @@ class Rekv:
         cache = self._paged(k_pages, v_pages, token_start, kv_len, page_table, q.shape[0])
         if prefix_pages.dim() != 1 or prefix_pages.dtype != torch.int32 or not prefix_pages.is_contiguous():
             raise ValueError("prefix_pages must be contiguous int32 with one dimension")
-        if n_prefix < 1 or prefix_pages.shape[0] * cache.page_size < n_prefix:
+        if not 1 <= n_prefix < 1 << 30 or prefix_pages.shape[0] * cache.page_size < n_prefix:
             raise ValueError(f"prefix_pages hold {prefix_pages.shape[0] * cache.page_size} tokens, n_prefix={n_prefix}")
         return self._attention_paged(q, cache, n_prefix, prefix_pages, max_kv, -1, 0, out)
 

@@ -50,6 +50,7 @@ def test_wrong_arguments_are_refused():
     k = torch.zeros((4, 2, 64), dtype=torch.bfloat16, device="cuda:0")
     batch = (kp, vp, start, kv, table)
     for kw, match in ((dict(sections=[8, 8]), "pairs"), (dict(sections=[40, -8]), "pairs"), (dict(base=1.0), "base"), (dict(sections=[]), "axes"),
+                      (dict(sections=[32, 1 << 32]), "pairs"), (dict(rotate=False, positions=ints([0] * 4)), "without"),
                       (dict(positions=torch.zeros(3, dtype=torch.int32, device="cuda:0")), "positions"), (dict(q_out=q), "q_out"),
                       (dict(q=q[:3]), "q"), (dict(q=q, q_out=q[:, :, :32]), "q_out")):
         with pytest.raises((ValueError, RekvError), match=match):
@@ -64,6 +65,29 @@ def test_wrong_arguments_are_refused():
     with pytest.raises(RekvError, match="head_dim"):
         Rekv(4, 2, 20, 16, "f32").rotate(torch.zeros((1, 4, 20), device="cuda:0"), ints([0]))
     assert torch.equal(kp.nan_to_num(), dev(b.k_pages, "bf16").nan_to_num())
+
+
+def test_arguments_beyond_32_bits_do_not_wrap():
+    b, r, (q, kp, vp, start, kv, table) = small()
+    want = r.attention_paged(q, kp, vp, start, kv, table)
+    for kw in (dict(window=1 << 32), dict(window=(1 << 31) - 1), dict(window=1 << 40, sinks=1 << 33), dict(max_kv=1 << 33), dict(max_kv=-5),
+               dict(window=1 << 30, max_kv=1 << 32)):
+        assert torch.equal(want, r.attention_paged(q, kp, vp, start, kv, table, **kw)), kw
+    narrow = r.attention_paged(q, kp, vp, start, kv, table, window=0, sinks=1 << 40)
+    assert torch.equal(want, narrow)
+    with pytest.raises((ValueError, RekvError)):
+        r.attention_shared_prefix(q, kp, vp, ints([1, 2]), (1 << 32) + 20, start, kv, table)
+
+
+def test_the_workspace_stays_bounded_by_a_wild_hint():
+    import ctypes
+    r = Rekv(28, 4, 128, 64)
+    L, n = rekv.lib(), ctypes.c_int64()
+    for tokens, seqs in ((1, 1), (64, 64), (196, 1), (500, 500)):
+        for max_kv in (1, 10 ** 4, 10 ** 6, (1 << 31) - 1):
+            for prefix in (0, 10 ** 6):
+                assert L.rekv_attention_paged_workspace(r._h, tokens, seqs, max_kv, -1, 0, prefix, ctypes.byref(n)) == 0
+                assert n.value <= 1 << 30, (tokens, seqs, max_kv, prefix, n.value)
 
 
 def test_a_small_workspace_is_refused_by_the_c_call():
