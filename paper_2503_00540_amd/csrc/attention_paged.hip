@@ -354,11 +354,12 @@ __device__ inline bool drop_nonfinite(uint32_t v_tile, int lane) {
     return true;
 }
 
-// The tiles [begin, end) of split `job.split`.
-__device__ inline void split_range(const PagedArgs& a, const Job& job, int n_tiles, int* begin, int* end) {
+// The tiles [begin, end) of split `job.split`; `runs` wavefronts divide them.
+__device__ inline void split_range(const PagedArgs& a, const Job& job, int n_tiles, int runs, int* begin, int* end) {
     int n = (n_tiles + job.n_splits - 1) / job.n_splits;
     const int least = job.own ? a.min_tiles : a.min_prefix_tiles;
     n = n > least ? n : least;
+    n = (n + runs - 1) / runs * runs;
     *begin = job.split * n;
     *end = *begin + n < n_tiles ? *begin + n : n_tiles;
 }
@@ -394,7 +395,7 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
     const bool wave_active = job.row0 + wave * WM < job.n_rows;
     const Tiles<BN> tiles = tiles_of<BM>(p, job, G);
     int t_begin, t_end;
-    split_range(a, job, tiles.n, &t_begin, &t_end);
+    split_range(a, job, tiles.n, 1, &t_begin, &t_end);
     const Src src(p, job, tiles, t_end, kvh, lane, wave);
     Places places;
     if (t_begin < t_end) src.fill(places, t_begin);      // (before the queries' loads, whose wait this one would be otherwise)
@@ -519,7 +520,7 @@ __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, co
     const int G = p.n_q_heads / p.n_kv_heads;
     const Tiles<BN> tiles = tiles_of<WM>(p, job, G);
     int begin, end;
-    split_range(a, job, tiles.n, &begin, &end);
+    split_range(a, job, tiles.n, WAVES, &begin, &end);
     const int n = end > begin ? end - begin : 0, each = n / WAVES, rest = n - each * WAVES;      // the first `rest` runs are one longer
     const int t_begin = begin + each * wave + (wave < rest ? wave : rest), t_end = t_begin + each + (wave < rest);
     const uint32_t k_tile = lds_addr_of(lds) + (uint32_t)wave * 2u * TILE_B, v_tile = k_tile + TILE_B;
@@ -753,7 +754,7 @@ __global__ __launch_bounds__(THREADS, D_MAX > 128 ? 1 : 2) void attn_paged_f32_k
         return;
     const Tiles<BN> tiles = tiles_of<F32_ROWS>(p, job, G);
     int t_begin, t_end;
-    split_range(a, job, tiles.n, &t_begin, &t_end);
+    split_range(a, job, tiles.n, WAVES, &t_begin, &t_end);
     const int row = job.row0 + r, tok = row / G, pos = job.p0 + tok;
     const bool row_ok = row < job.n_rows;
     const int64_t q_row = (int64_t)(job.token0 + tok) * p.n_q_heads + kvh * G + (row - tok * G);
@@ -963,7 +964,7 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     // 18.7 with one, 17.5 with three).
     plan.min_tiles = few ? 8 : 4;
     int64_t s = places / (busy * n_kv_heads);
-    if (s > tiles / plan.min_tiles) s = tiles / plan.min_tiles;
+    if (s > up(tiles, plan.min_tiles)) s = up(tiles, plan.min_tiles);
     // Where lone rows all but fill it, their lengths differ: pieces of one size, LONG tiles, spread the longer ones (64 users of 1 to 8,192
     // tokens at 64/8/128: 221 us whole, 207, 199, 199, 205 in pieces of 96, 64, 48, 32).
     constexpr int64_t LONG = 64, MOST_PIECES = 64;
