@@ -1,5 +1,5 @@
-// Attention of a ragged batch over a paged cache, bf16: sliding windows with first tokens that stay visible, and batches that
-// share a long prefix.
+// Attention of a ragged batch over a paged cache: sliding windows with first tokens that stay visible, and batches that share a
+// long prefix.
 //
 //   o = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m),  s_j = scale q.k_j,  over the keys j a token sees (paged.h)
 //
@@ -10,8 +10,14 @@
 // Rows are stacked as in attention_bf16.hip, the G query heads of a KV head token by token, so a K/V tile in LDS
 // serves them all; a prefix shared by the batch is walked by blocks of all sequences' rows, so that one user's few rows do not
 // read it for themselves.  Operand layouts, the four LDS stages per tensor and the order of a step are those of attention_bf16.hip.
-// What differs is where tiles come from: 32 keys lie in one or two pages, whose numbers come through the scalar cache a
-// step before the loads that need them.
+// What differs is where tiles come from: 32 keys lie in one or two pages, and the places of 64 tiles are worked out at once.
+//
+// What bounds it (28/4/128, pages of 64 to 256 unless said).  Long prompts: the matrix cores at the clock the chip grants them,
+// 1.04 to 1.07 PFLOP/s for 8,192 tokens (451 to 470 us; a library GEMM of 8,192^3 reaches 1.24), as attention_bf16.hip.  Many users' decode
+// steps: HBM, 5.5 TB/s for 64 users of 1 to 8,192 tokens at 64/8/128 (199 us), 6.1 where all have 4,096.  One user's: round trips; a
+// workgroup of a 15,000-token window spends (us) 0.4 on finding its sequence, 1.3 on the page table, 0.8 to the first tile, 3.0 on two tiles
+// per wavefront and 1.2 on the merge in LDS, the joining launch 3.9, 15.7 in all.  A live frame over 3,136 keys: 0.8, 0.8 and 3.4 to the
+// first tiles, 0.97 per tile with two workgroups per CU (0.67 with one), 1.8 to write.
 #include "attention_mfma.h"
 #include "paged.h"
 
@@ -288,7 +294,8 @@ struct Rows {
     }
 
     // The values that drop_nonfinite took out of tiles [t0, t1), for the rows that do see them: from memory, key by key.
-    __device__ __attribute__((always_inline)) void add_nonfinite(const PagedProblem& p, const Job& job, const Tiles<BN>& tiles, int t0, int t1, int kvh, int hh) {
+    __device__ __attribute__((always_inline)) void add_nonfinite(const PagedProblem& p, const Job& job, const Tiles<BN>& tiles, int t0, int t1,
+                                                                 int kvh, int hh) {
         if (!ok) return;
         const float mr = (m_ref == -INFINITY) ? 0.f : m_ref;
         const int page = (int)p.b.by_page.d;
@@ -507,8 +514,8 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
 }
 
 // A block of 32 rows, as a decode step's: its four wavefronts divide the KEYS, each walks its run of tiles through a K and a V tile
-// of its own in LDS without a barrier, and their results meet in LDS.  STREAM: non-temporal loads, where nobody else reads the keys (64 users'
-// decode step 201 us so, 224 with cached loads).
+// of its own in LDS without a barrier, and their results meet in LDS.  STREAM: non-temporal loads, where nobody else reads the keys (64
+// users' decode step 201 us so, 224 with cached loads; a live frame over 3,136 keys, which 43 blocks read, 40 and 31).
 template <int D, bool TWO_PAGES, bool STREAM>
 __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, const Job& job, int kvh, unsigned char* lds, f32x2 (*ml)[WM]) {
     typedef Source<D, TWO_PAGES, 1, STREAM> Src;
@@ -616,8 +623,8 @@ __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, co
     }
 }
 
-// ROW_BLOCKS: all by blocks of 128 rows.  KEY_BLOCKS, STREAMED: the sequences' own keys by blocks of 32 rows, a prefix shared by the batch still by blocks of 128 (a batch of 42 rows over 3,136
-// prefix tokens takes 11.1 us so, 10.8 to 11.6 by blocks of 32).
+// ROW_BLOCKS: all by blocks of 128 rows.  KEY_BLOCKS, STREAMED: the sequences' own keys by blocks of 32 rows, a prefix shared by the
+// batch still by blocks of 128 (42 rows over 3,136 prefix tokens take 11.1 us so, 10.8 to 11.6 by blocks of 32).
 template <int D, bool TWO_PAGES, int HOW>
 __global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
     constexpr bool FEW = HOW != ROW_BLOCKS;
@@ -629,7 +636,8 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
     const bool prefix = L < a.prefix_blocks * a.prefix_splits;
     Job job;
     if (FEW && !prefix) {
-        if (find_own_job<WM>(a.p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job)) keys_block<D, TWO_PAGES, HOW == STREAMED>(a, job, kvh, lds, ml);
+        if (find_own_job<WM>(a.p, a.prefix_blocks, a.prefix_splits, a.blocks, a.splits, L, lane, &job))
+            keys_block<D, TWO_PAGES, HOW == STREAMED>(a, job, kvh, lds, ml);
         return;
     }
     if (prefix ? find_prefix_job<BM>(a.p, a.prefix_blocks, a.prefix_splits, L, &job)
@@ -637,9 +645,10 @@ __global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
         rows_block<D, TWO_PAGES>(a, job, kvh, lds_addr_of(lds), &sh_dropped);
 }
 
-// Joins the partial results of the rows (token, head).  TPR threads own four dimensions each of a row; the slots of a row are
-// spread over a.n_slots / per_group thread groups, whose sums meet in LDS, so that a few rows of many slots (one user) are not
-// read one after the other.  Slots of no keys hold the maximum -inf and are not read.
+// Joins the partial results of the rows (token, head).  tpr threads own four dimensions each of a row; the slots of a row are
+// spread over `groups` sets of them, whose sums meet in LDS, so that a few rows of many slots (one user) are not read one after the
+// other: 28 rows of 58 slots 9.3 us with 256 threads a row and a maximum waited for before its sums, 3.9 so.  Slots of no keys hold the
+// maximum -inf; what else they hold is not used.
 constexpr int MOST_MERGE_THREADS = 1024;
 template <bool BF16>
 __global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(PagedArgs a, int tpr, int groups, int rows_per_block) {
@@ -718,9 +727,9 @@ __global__ __launch_bounds__(MOST_MERGE_THREADS) void attn_paged_merge_kernel(Pa
 }
 
 // ---- fp32: true fp32 products and sums on the matrix cores, operands straight from memory as in attention_f32.hip.  Head sizes between
-// 64, 128 and 256 (D_MAX) are padded with zeros in the registers.  A workgroup's four wavefronts share 16 stacked rows and take the 32-key tiles in turn; their (maximum, sum, O)
-// meet in LDS.  Bound, at the sizes that fp32 serves, by the round trips to the first key.  The tiny configuration's ragged batch
-// (5 sequences, window 77) takes 8.1 us, on the vector ALU below 21.5.
+// 64, 128 and 256 (D_MAX) are padded with zeros in the registers.  A workgroup's four wavefronts share 16 stacked rows and take the
+// 32-key tiles in turn; their (maximum, sum, O) meet in LDS.  Bound, at the sizes that fp32 serves, by the round trips to the first key.  The tiny configuration's ragged batch
+// (5 sequences, window 77) takes 8.1 us, 21.5 on the vector ALU.
 constexpr int F32_ROWS = 16;
 
 // All four lanes (q, q + 16, q + 32, q + 48) of a query combine a value.
