@@ -942,6 +942,7 @@ __global__ __launch_bounds__(THREADS, D_MAX > 128 ? 1 : 2) void attn_paged_f32_k
 }
 
 int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
+constexpr int64_t MOST_PARTIALS = (int64_t)512 << 20;      // bytes of a prefix's partial results
 constexpr int64_t PLACES = 512;       // workgroups of a bf16 launch that the chip holds: two per CU
 
 }  // namespace
@@ -951,7 +952,7 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     const int64_t G = n_q_heads / n_kv_heads, all_rows = n_tokens * G;
     const bool bf16 = dtype == REKV_BF16;
     PagedPlan plan;
-    int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
+    const int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
     // Blocks of 32 rows start and end sooner but fetch every tile four times as often: they take the sequences' own keys where few rows of
     // a sequence share them, and where there is little to do in all: up to SMALL tiles of 128 rows per place.  28/4/128 and 14/2/64, as
     // blocks of 128 and of 32 rows (us): a prompt of 196 tokens 13.8 and 8.6, 16 tokens over 3,000 17.8 and 14.1, a prompt of 1,000 34.7
@@ -960,14 +961,51 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     constexpr int64_t SMALL = 6;
     const int64_t row_blocks = up(all_rows, BM) > n_seqs ? up(all_rows, BM) : n_seqs;
     const bool lone = all_rows <= n_seqs * WM;
-    const bool few = bf16 && (lone || row_blocks * n_kv_heads * up(keys + n_prefix, BN) <= SMALL * PLACES);
+    const bool small = row_blocks * n_kv_heads * up(keys + n_prefix, BN) <= SMALL * PLACES;
+    const bool few = bf16 && (lone || small);
+
+    // Blocks of 128 rows in `jobs` times n workgroups over `tiles` tiles, in us: rounds of workgroups, each of about 8 us and tau a tile; and
+    // what a partial result of every row takes to write and read again.
+    const double tau = head_dim == 128 ? 0.8 : 0.5, slot_us = (double)(n_tokens * n_q_heads * (head_dim + 2)) * 8.0 / 3.5e6;
+    auto rows_us = [&](double jobs, int64_t tiles, int64_t n) { return ceil(jobs * (double)n / PLACES) * ((double)tiles / (double)n * tau + 8.0); };
+    // blocks that ragged sequences fill, about; uneven over the XCDs
+    const double own_jobs = (n_seqs == 1 ? (double)row_blocks : 1.15 * ((double)all_rows / BM + 0.5 * (double)n_seqs)) * (double)n_kv_heads;
+
+    // A prefix is computed for the batch at once, by full blocks of all sequences' rows whose results are joined with the own keys', or
+    // walked by each sequence's own blocks.  Measured, walked and at once (us, 28/4/128, a prefix of 4,608): 64 sequences of 12 tokens 119
+    // and 77, of 24 211 and 132, of 32 228 and 158, of 48 260 and 249, of 64 280 and 305, 24 of 40 128 and 86, 16 of 12 45 and 36.
+    plan.prefix_blocks = plan.prefix_splits = 0;
+    plan.min_prefix_tiles = 4;
+    bool together = n_prefix > 0 && (bf16 ? lone : all_rows < n_seqs * (F32_ROWS / 2));
+    const int64_t prefix_rows = bf16 ? BM : F32_ROWS, prefix_tiles = up(n_prefix, BN);
+    if (n_prefix > 0 && (together || (bf16 && !small))) {
+        plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
+        plan.prefix_splits = 1;
+        const double jobs = (double)plan.prefix_blocks * (double)n_kv_heads;
+        // Lone rows' workgroups are short and run beside these: half a place each (64 users over 25,088 tokens at 28/4/128, us: 48.5 with 24
+        // splits, as this gives, 56.0 with 32, 50.6 with 16).
+        const double beside = lone ? 0.5 * (double)(n_seqs * n_kv_heads) : 0.0;
+        double best = 1e30;
+        const int64_t most = MOST_PARTIALS / (n_tokens * n_q_heads * (head_dim + 2) * 4);
+        for (int64_t n = 1; n == 1 || (n <= PLACES && n <= most && n * plan.min_prefix_tiles <= prefix_tiles); ++n) {
+            const double us = rows_us(jobs + beside / (double)n, prefix_tiles, n) + (double)n * slot_us;
+            if (us < best) {
+                best = us;
+                plan.prefix_splits = (int32_t)n;
+            }
+        }
+        if (!together) {
+            const int64_t s = PLACES / (row_blocks * n_kv_heads), tiles = up(keys + n_prefix, BN);
+            const double walked = rows_us(own_jobs, tiles, s > 1 ? s : 1) + (s > 1 ? (double)s * slot_us + 4.0 : 0.0);
+            together = best + rows_us(own_jobs, up(keys, BN), 1) + slot_us + 4.0 < walked;
+            if (!together) plan.prefix_blocks = plan.prefix_splits = 0;
+        }
+    }
+
     plan.how = !few ? ROW_BLOCKS : lone ? STREAMED : KEY_BLOCKS;
     plan.rows = !bf16 ? F32_ROWS : few ? WM : BM;
-    const int64_t prefix_rows = bf16 ? BM : plan.rows;
     plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
     const int64_t places = bf16 ? PLACES : 1024, busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
-    // Rows that fill blocks by themselves walk the prefix in their own blocks.
-    const bool together = n_prefix > 0 && all_rows < n_seqs * (prefix_rows / 2);
     const int64_t tiles = up(together ? keys : keys + n_prefix, BN);
     // As many splits as fill the chip, each of two tiles a wavefront at least (a user's window of 15,000 tokens at 28/4/128 takes 16.7 us so,
     // 18.7 with one, 17.5 with three).
@@ -982,17 +1020,6 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
         plan.min_tiles = (int32_t)LONG;
     }
     plan.splits = (int32_t)(s < 1 ? 1 : s);
-    plan.prefix_blocks = plan.prefix_splits = 0;
-    plan.min_prefix_tiles = 4;
-    if (together) {
-        // beside the own keys' workgroups, which are short: half a place each (64 users over 25,088 tokens at 28/4/128, us: 48.5 with 24 splits, as
-        // this gives, 56.0 with 32, 50.6 with 16)
-        const int64_t left = places - busy * n_kv_heads / 2, prefix_tiles = up(n_prefix, BN);
-        plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
-        int64_t n = (left > places / 4 ? left : places / 4) / (plan.prefix_blocks * n_kv_heads);
-        if (n > prefix_tiles / plan.min_prefix_tiles) n = prefix_tiles / plan.min_prefix_tiles;
-        plan.prefix_splits = (int32_t)(n < 1 ? 1 : n);
-    }
     plan.workspace_bytes = plan.slots() > 1 ? n_tokens * n_q_heads * plan.slots() * (head_dim + 2) * 4 : 0;
     return plan;
 }
