@@ -954,14 +954,15 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     PagedPlan plan;
     const int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
     // Blocks of 32 rows start and end sooner but fetch every tile four times as often: they take the sequences' own keys where few rows of
-    // a sequence share them, and where there is little to do in all: up to SMALL tiles of 128 rows per place.  28/4/128 and 14/2/64, as
+    // a sequence share them, and where there is little to do in all: up to SMALL tiles of 128 rows per place (causal ones half).  28/4/128 and 14/2/64, as
     // blocks of 128 and of 32 rows (us): a prompt of 196 tokens 13.8 and 8.6, 16 tokens over 3,000 17.8 and 14.1, a prompt of 1,000 34.7
     // and 28.5, a live frame over 3,136 at 14/2/64 22.1 and 16.8; the other way 4 x 8 tokens over 8,000 18.7 and 20.4 (7.8 tiles a place),
     // 32 x 16 over 3,000 42 and 58 (23), 4 live frames of 64/8/128 53 and 64 (23).
-    constexpr int64_t SMALL = 6;
+    constexpr int64_t SMALL = 7;
     const int64_t row_blocks = up(all_rows, BM) > n_seqs ? up(all_rows, BM) : n_seqs;
     const bool lone = all_rows <= n_seqs * WM;
-    const bool small = row_blocks * n_kv_heads * up(keys + n_prefix, BN) <= SMALL * PLACES;
+    const int64_t causal = n_tokens / n_seqs < keys ? n_tokens / n_seqs : keys;
+    const bool small = row_blocks * n_kv_heads * up(keys + n_prefix - causal / 2, BN) <= SMALL * PLACES;
     const bool few = bf16 && (lone || small);
 
     // Blocks of 128 rows in `jobs` times n workgroups over `tiles` tiles, in us: rounds of workgroups, each of about 8 us and tau a tile; and
