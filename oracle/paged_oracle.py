@@ -57,9 +57,10 @@ def visible(p, n_keys, window, sinks):
     return [j for j in range(min(p + 1, n_keys)) if window is None or p - j < window or j < sinks]
 
 
-def attention(q, k_pages, v_pages, token_start, kv_len, table, scale, window=None, sinks=0, prefix_pages=(), n_prefix=0):
+def attention(q, k_pages, v_pages, token_start, kv_len, table, scale, window=None, sinks=0, prefix_pages=(), n_prefix=0, every=1):
     """[n_tokens, Hq, D] and the same with |v| in the place of v (what a rounding of the probabilities can move); rows of
-    no sequence are NaN, rows that see nothing 0."""
+    no sequence are NaN, rows that see nothing 0.  every > 1: only so many tokens of a sequence, its first and last among them; the
+    others are NaN too."""
     q = np.asarray(q, dtype=np.float64)
     size, hkv = k_pages.shape[1:3]
     g = q.shape[1] // hkv
@@ -67,7 +68,7 @@ def attention(q, k_pages, v_pages, token_start, kv_len, table, scale, window=Non
     first = [row_of(prefix_pages, j, size) for j in range(n_prefix)]
     for s in range(len(kv_len)):
         n = token_start[s + 1] - token_start[s]
-        for i in range(n):
+        for i in sorted({*range(0, n, every), n - 1} if n else ()):
             p, t = kv_len[s] - n + i, token_start[s] + i
             at = first + [row_of(table[s], j, size) for j in visible(p, len(table[s]) * size, window, sinks)]
             out[t] = spread[t] = 0.0

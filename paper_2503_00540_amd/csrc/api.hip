@@ -976,4 +976,13 @@ int32_t rekv_internal_attention_key_groups(int32_t n_q_heads, int32_t n_kv_heads
                                                  in_place)).key_groups;
 }
 
+// And of attention over a paged cache.  out: form (0: blocks of 128 rows, 1 and 2: of 32; fp32 0), rows per block, blocks and splits of the
+// own keys, blocks and splits of a prefix computed for the batch at once, workspace bytes, workgroups.
+void rekv_internal_paged_plan(int32_t dtype, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_tokens, int32_t n_seqs,
+                              int32_t max_kv, int32_t window, int32_t sinks, int32_t n_prefix, int64_t out[8]) {
+    const rekv::PagedPlan p = rekv::attn_paged_plan(dtype, n_q_heads, n_kv_heads, head_dim, n_tokens, n_seqs, max_kv, window, sinks, n_prefix);
+    out[0] = p.how; out[1] = p.rows; out[2] = p.blocks; out[3] = p.splits; out[4] = p.prefix_blocks; out[5] = p.prefix_splits;
+    out[6] = p.workspace_bytes; out[7] = ((int64_t)p.prefix_blocks * p.prefix_splits + (int64_t)p.blocks * p.splits) * n_kv_heads;
+}
+
 }  // extern "C"

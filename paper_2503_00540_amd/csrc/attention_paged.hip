@@ -974,7 +974,8 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
 
     // A prefix is computed for the batch at once, by full blocks of all sequences' rows whose results are joined with the own keys', or
     // walked by each sequence's own blocks.  Measured, walked and at once (us, 28/4/128, a prefix of 4,608): 64 sequences of 12 tokens 119
-    // and 77, of 24 211 and 132, of 32 228 and 158, of 48 260 and 249, of 64 280 and 305, 24 of 40 128 and 86, 16 of 12 45 and 36.
+    // and 77, of 24 211 and 132, of 32 228 and 158, of 48 260 and 249, of 64 280 and 305, 24 of 40 128 and 86, 16 of 12 45 and 36.  The estimate is off
+    // by a tenth where the two are alike: of these it takes the slower one at 48 and at 64 tokens.
     plan.prefix_blocks = plan.prefix_splits = 0;
     plan.min_prefix_tiles = 4;
     bool together = n_prefix > 0 && (bf16 ? lone : all_rows < n_seqs * (F32_ROWS / 2));

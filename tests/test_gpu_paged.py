@@ -12,7 +12,10 @@ HEADS = [(14, 2, 64, "bf16"), (28, 4, 128, "bf16"), (8, 8, 64, "bf16"), (4, 1, 6
          (6, 2, 80, "f32"), (2, 1, 256, "f32")]
 
 
-def attend(b, window=None, sinks=0, max_kv=None, r=None):
+LONG = 10 ** 6          # as a hint: launches of few rows are no longer taken for short ones
+
+
+def attend(b, window=None, sinks=0, max_kv=None, r=None, every=1):
     r = r or Rekv(b.hq, b.hkv, b.d, b.page, b.dtype)
     q, kp, vp, start, kv, table = b.device()
     out = torch.full_like(q, 7.0)
@@ -22,14 +25,16 @@ def attend(b, window=None, sinks=0, max_kv=None, r=None):
         got = r.attention_paged(q, kp, vp, start, kv, table, max_kv=max_kv, window=window, sinks=sinks, out=out)
     torch.cuda.synchronize()
     assert got is out
-    check(out, b, window, sinks, before=torch.full_like(q, 7.0))
+    check(out, b, window, sinks, before=torch.full_like(q, 7.0), every=every)
 
 
 @pytest.mark.parametrize("heads", HEADS)
 @pytest.mark.parametrize("page", [1, 5, 16, 32, 48, 196])
 def test_ragged_batches(heads, page):
     # decode steps, short and longer new parts, a sequence without new tokens, one without any, the whole sequence new
-    attend(Batch([1, 7, 0, 40, 0, 1, 33], [1, 130, 50, 40, 0, 300, 65], page, *heads, pad=3))
+    b = Batch([1, 7, 0, 40, 0, 1, 33], [1, 130, 50, 40, 0, 300, 65], page, *heads, pad=3)
+    attend(b)
+    attend(b, max_kv=LONG)
 
 
 @pytest.mark.parametrize("heads", HEADS)
@@ -44,12 +49,30 @@ def test_windows_and_sinks(heads, window, sinks):
 @pytest.mark.parametrize("heads", [HEADS[1], HEADS[0], HEADS[3]])
 @pytest.mark.parametrize("new,kv,page", [(1, 9000, 64), (1, 2500, 7), (3, 4099, 196), (200, 5000, 144)])
 def test_long_sequences_are_split(heads, new, kv, page):
-    b = Batch([new], [kv], page, *heads)
-    attend(b)
-    attend(b, max_kv=1)               # the hint splits the work, nothing else
-    attend(b, max_kv=10 ** 9)
+    b, every = Batch([new], [kv], page, *heads), 1 if new < 10 else 19
+    attend(b, every=every)
+    attend(b, max_kv=1, every=every)                  # the hint splits the work, nothing else
+    attend(b, max_kv=10 ** 9, every=every)
     b.lost_pages(1500, 40)
-    attend(b, 1500, 40)
+    attend(b, 1500, 40, every=every)
+
+
+@pytest.mark.parametrize("heads", [HEADS[0], HEADS[1]])
+@pytest.mark.parametrize("page", [5, 16, 48, 144])
+def test_many_rows(heads, page):
+    """Enough rows for blocks of 128 whose results go straight to the output: prompts, windows inside and beyond a block, sinks."""
+    b = Batch([1200, 300, 1], [1500, 410, 700], page, *heads, pad=4)
+    attend(b, every=61)
+    attend(b, 700, 20, every=61)
+    attend(b, 1400, 0, every=61)
+
+
+@pytest.mark.parametrize("heads", [HEADS[0], HEADS[1]])
+@pytest.mark.parametrize("seqs,new,n_prefix,page", [(3, 200, 5000, 64), (40, 30, 2100, 144), (24, 100, 2500, 7), (70, 3, 3000, 16)])
+def test_prefixes_of_many_rows(heads, seqs, new, n_prefix, page):
+    """Prefixes at once in several pieces and walked, over more tiles than are placed at a time, sequences of more than a lane each."""
+    b = Batch([new if s % 3 else max(new // 2, 1) for s in range(seqs)], [new + s for s in range(seqs)], page, *heads, n_prefix=n_prefix, pad=2)
+    attend(b, every=max(new // 2, 2))
 
 
 @pytest.mark.parametrize("heads", HEADS)
@@ -87,11 +110,12 @@ def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(heads, valu
     want, spread = b.want()
     r = Rekv(*heads[:3], 16, b.dtype)
     q, kp, vp, start, kv, table = b.device()
-    got = r.attention_paged(q, kp, vp, start, kv, table).double().cpu().numpy()
-    assert np.array_equal(np.isfinite(got), np.isfinite(want)) and np.array_equal(np.isnan(got), np.isnan(want))
-    assert (~np.isfinite(want)).any()
     fine = np.isfinite(want)
-    assert (np.abs(got - want)[fine] <= b.tolerance(want, np.abs(spread))[fine]).all()
+    assert not fine.all()
+    for max_kv in (None, LONG):
+        got = r.attention_paged(q, kp, vp, start, kv, table, max_kv=max_kv).double().cpu().numpy()
+        assert np.array_equal(np.isfinite(got), fine) and np.array_equal(np.isnan(got), np.isnan(want))
+        assert (np.abs(got[fine] - want[fine]) <= b.tolerance(want, np.abs(spread))[fine]).all()
 
 
 @pytest.mark.parametrize("heads", [HEADS[0], HEADS[1], HEADS[3]])
@@ -100,9 +124,10 @@ def test_a_key_that_is_nan_stays_with_the_rows_that_see_it(heads):
     b.k_pages[b.table[0][170 // 16], 170 % 16, 0] = np.nan
     r = Rekv(*heads[:3], 16, b.dtype)
     q, kp, vp, start, kv, table = b.device()
-    got = r.attention_paged(q, kp, vp, start, kv, table)
     g = heads[0] // heads[1]
-    assert torch.isfinite(got[:30]).all() and torch.isnan(got[30:, :g]).all() and torch.isfinite(got[30:, g:]).all()
+    for max_kv in (None, LONG):
+        got = r.attention_paged(q, kp, vp, start, kv, table, max_kv=max_kv)
+        assert torch.isfinite(got[:30]).all() and torch.isnan(got[30:, :g]).all() and torch.isfinite(got[30:, g:]).all()
 
 
 def test_large_scores():
