@@ -18,6 +18,8 @@
 // workgroup of a 15,000-token window spends (us) 0.4 on finding its sequence, 1.3 on the page table, 0.8 to the first tile, 3.0 on two tiles
 // per wavefront and 1.2 on the merge in LDS, the joining launch 3.9, 15.7 in all.  A live frame over 3,136 keys: 0.8, 0.8 and 3.4 to the
 // first tiles, 0.97 per tile with two workgroups per CU (0.67 with one), 1.8 to write.
+#include <float.h>
+
 #include "attention_mfma.h"
 #include "paged.h"
 
@@ -361,6 +363,10 @@ __device__ inline bool drop_nonfinite(uint32_t v_tile, int lane) {
     return true;
 }
 
+// What a partial result's exponents refer to: -inf where it has no keys, and only there.  Scores that are all NaN leave a NaN sum under
+// no maximum, which must not pass for none.
+__device__ inline float part_max(float m, float l) { return l == 0.f ? -INFINITY : fmaxf(m, -FLT_MAX); }
+
 // The tiles [begin, end) of split `job.split`; `runs` wavefronts divide them.
 __device__ inline void split_range(const PagedArgs& a, const Job& job, int n_tiles, int runs, int* begin, int* end) {
     int n = (n_tiles + job.n_splits - 1) / job.n_splits;
@@ -509,7 +515,7 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
                 for (int j = 0; j < 16; j += 4)
                     *reinterpret_cast<f32x4*>(out + db * 32 + j * 2) = f32x4{r.o[db][j], r.o[db][j + 1], r.o[db][j + 2], r.o[db][j + 3]};
         }
-        if (hh == 0) *reinterpret_cast<f32x2*>(a.part_ml + to * 2) = f32x2{l_tot != 0.f ? r.m_ref : -INFINITY, l_tot};
+        if (hh == 0) *reinterpret_cast<f32x2*>(a.part_ml + to * 2) = f32x2{part_max(r.m_ref, l_tot), l_tot};
     }
 }
 
@@ -582,14 +588,14 @@ __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, co
     // ---- the wavefronts' results meet in LDS, each scaled to the common maximum, in its own tiles; 16-byte chunk c of row i lies at
     // chunk position c ^ i, so that writes (a row per lane) and reads (a row per CPR lanes) touch all banks
     const float l_tot = pair_sum(r.l);
-    if (hh == 0) ml[wave][col] = f32x2{l_tot != 0.f ? r.m_ref : -INFINITY, l_tot};
+    if (hh == 0) ml[wave][col] = f32x2{part_max(r.m_ref, l_tot), l_tot};
     __syncthreads();
     const int n_rows = job.n_rows - job.row0 < WM ? job.n_rows - job.row0 : WM;
     if (r.ok) {
         float m_all = ml[0][col][0];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m_all = fmaxf(m_all, ml[w][col][0]);
-        const float f = l_tot == 0.f ? 0.f : __builtin_amdgcn_exp2f(r.m_ref - m_all);
+        const float f = l_tot == 0.f ? 0.f : __builtin_amdgcn_exp2f(part_max(r.m_ref, l_tot) - m_all);
         f32x4* mine = reinterpret_cast<f32x4*>(lds + (size_t)wave * 2 * TILE_B);
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -913,7 +919,7 @@ __global__ __launch_bounds__(THREADS, D_MAX > 128 ? 1 : 2) void attn_paged_f32_k
 #pragma unroll
         for (int i = 0; i < 4; ++i) o_lds[wave][b * 4 + i][lane] = f32x4{o[b][0][i], o[b][1][i], o[b][2][i], o[b][3][i]};
     if (g == 0) {
-        m_lds[wave][r] = l != 0.f ? m : -INFINITY;
+        m_lds[wave][r] = part_max(m, l);
         l_lds[wave][r] = l;
     }
     __syncthreads();

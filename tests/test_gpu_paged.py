@@ -130,6 +130,28 @@ def test_a_key_that_is_nan_stays_with_the_rows_that_see_it(heads):
         assert torch.isfinite(got[:30]).all() and torch.isnan(got[30:, :g]).all() and torch.isfinite(got[30:, g:]).all()
 
 
+@pytest.mark.parametrize("heads", [HEADS[0], HEADS[1], HEADS[3]])
+@pytest.mark.parametrize("new,kv,prefix", [([1, 2], [5000, 900], 0), ([40, 3], [5000, 900], 0), ([1, 1, 1], [9, 40, 200], 3000), ([40, 30], [300, 90], 3000)])
+def test_rows_of_nothing_but_nan_scores_are_nan(heads, new, kv, prefix):
+    """A query that is NaN, and a lone key that is: however the keys are split, the row does not pass for one that sees nothing."""
+    b = Batch(new, kv, 16, *heads, n_prefix=prefix)
+    bad = new[0] - 1                                 # the first sequence's last token
+    b.q[bad, -1, 5] = np.nan
+    r = Rekv(*heads[:3], 16, b.dtype)
+    q, kp, vp, start, kv_len, table = b.device()
+    pages = ints(b.prefix_pages) if prefix else None
+    for max_kv in (None, LONG):
+        got = r.attention_shared_prefix(q, kp, vp, pages, prefix, start, kv_len, table, max_kv=max_kv) if prefix else \
+            r.attention_paged(q, kp, vp, start, kv_len, table, max_kv=max_kv)
+        nan = torch.isnan(got)
+        assert nan[bad, -1].all() and int(nan.sum()) == heads[2]
+    if not prefix:
+        b.k_pages[b.table[0][(kv[0] - 1) // 16], (kv[0] - 1) % 16, 0] = np.nan
+        for sinks in (0, 30):
+            got = r.attention_paged(q, dev(b.k_pages, b.dtype), vp, start, kv_len, table, max_kv=LONG, window=1, sinks=sinks)
+            assert torch.isnan(got[bad, :heads[0] // heads[1]]).all() and torch.isfinite(got[new[0]:]).all()
+
+
 def test_large_scores():
     for heads in (HEADS[1], HEADS[3]):
         # scores of hundreds: a single key takes the row; the running maximum moves far
