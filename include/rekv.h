@@ -393,7 +393,8 @@ rekv_status rekv_offload_join(rekv_ctx* ctx, void* stream);
  * for others nor written.  Lengths and tables are read on the device, so a captured call may
  * be replayed with others.  What they say is never followed out of bounds: page numbers
  * outside [0, n_pages) are taken as the nearest page when read and skipped when written.
- * n_pages * page_size and max_pages * page_size are below 2^30; the arrays may be larger than 4 GiB.
+ * n_pages * page_size and max_pages * page_size are below 2^30, n_tokens * Hq too, n_seqs below
+ * 2^24 and a token's keys below 64 MiB; the arrays may be larger than 4 GiB.
  */
 typedef struct {
     void* k_pages;
@@ -450,7 +451,9 @@ rekv_status rekv_append_kv(rekv_ctx* ctx, const rekv_paged* cache, const rekv_ro
  * Causal attention of a batch's new tokens over their sequences' pages, whole or through a sliding
  * window beside the first tokens, which stay visible (sinks).  The token at index p sees index j iff
  *   j <= p  and  (window < 0  or  p - j < window  or  j < sinks).
- * A token that sees nothing (window 0 and no sinks, a negative index) gets zeros.
+ * A token that sees nothing (window 0 and no sinks, a negative index) gets zeros, as one whose
+ * scores are all -infinity does.  Batches that would take 2^24 workgroups or a workspace of
+ * more than 64 GiB are refused.
  *   q, out     [n_tokens, Hq, D]; the new tokens' keys and values are already in the pages
  *   window     tokens, the token itself among them; negative: no window (sinks is then without effect)
  *   max_kv     about the largest kv_len, for the split of the work only: any value gives right results

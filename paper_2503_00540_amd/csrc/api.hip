@@ -751,6 +751,8 @@ static rekv_status paged_batch(rekv_ctx* c, const char* fn, const rekv_paged* in
     if ((int64_t)in->n_pages * in->page_size >= (1 << 30) || (int64_t)in->max_pages * in->page_size >= (1 << 30))
         return fail(c, REKV_ERR_UNSUPPORTED, "%s: %d pages, %d of them per sequence, of %d tokens: below 2^30 tokens each", fn, in->n_pages,
                     in->max_pages, in->page_size);
+    if ((int64_t)c->shape.n_kv_heads * c->shape.head_dim * (int64_t)elem_size(c) >= 1 << 26)          // 32 rows: 32-bit offsets
+        return fail(c, REKV_ERR_UNSUPPORTED, "%s: the %d key heads of a token must be below 64 MiB", fn, c->shape.n_kv_heads);
     if ((int64_t)in->n_tokens * c->shape.n_q_heads >= (1 << 30) || in->n_seqs >= (1 << 24))
         return fail(c, REKV_ERR_UNSUPPORTED, "%s: %d tokens of %d sequences are too many", fn, in->n_tokens, in->n_seqs);
     b->k_pages = in->k_pages; b->v_pages = in->v_pages;
@@ -862,9 +864,17 @@ rekv_status rekv_append_kv(rekv_ctx* c, const rekv_paged* cache, const rekv_rota
 
 constexpr int32_t MOST_KEYS = 1 << 30;       // no sequence is longer: a larger window is none
 
-static rekv::PagedPlan paged_plan(rekv_ctx* c, int64_t n_tokens, int64_t n_seqs, int32_t max_kv, int32_t window, int32_t sinks, int64_t n_prefix) {
-    return rekv::attn_paged_plan(c->shape.dtype, c->shape.n_q_heads, c->shape.n_kv_heads, c->shape.head_dim, n_tokens, n_seqs,
-                                 max_kv < 1 ? 1 : max_kv < MOST_KEYS ? max_kv : MOST_KEYS, window < MOST_KEYS ? window : -1, sinks, n_prefix);
+// A launch has below 2^32 threads: 256 for each workgroup, and for the joining of partial results one per 32 bytes of them at most, or two
+// where the rows do not divide a workgroup.
+static rekv_status paged_plan(rekv_ctx* c, const char* fn, int64_t n_tokens, int64_t n_seqs, int32_t max_kv, int32_t window, int32_t sinks,
+                              int64_t n_prefix, rekv::PagedPlan* plan) {
+    *plan = rekv::attn_paged_plan(c->shape.dtype, c->shape.n_q_heads, c->shape.n_kv_heads, c->shape.head_dim, n_tokens, n_seqs,
+                                  max_kv < 1 ? 1 : max_kv < MOST_KEYS ? max_kv : MOST_KEYS, window < MOST_KEYS ? window : -1, sinks, n_prefix);
+    const int64_t jobs = ((int64_t)plan->prefix_blocks * plan->prefix_splits + (int64_t)plan->blocks * plan->splits) * c->shape.n_kv_heads;
+    if (jobs >= 1 << 24 || plan->workspace_bytes > (int64_t)1 << 36)
+        return fail(c, REKV_ERR_UNSUPPORTED, "%s: %lld tokens of %lld sequences would take %lld workgroups and a workspace of %lld bytes; call it on parts of the batch",
+                    fn, (long long)n_tokens, (long long)n_seqs, (long long)jobs, (long long)plan->workspace_bytes);
+    return REKV_OK;
 }
 
 static rekv_status attention_paged(rekv_ctx* c, const char* fn, const rekv_paged* cache, const void* q, const int32_t* prefix_pages,
@@ -878,12 +888,12 @@ static rekv_status attention_paged(rekv_ctx* c, const char* fn, const rekv_paged
     memset(&p, 0, sizeof(p));
     rekv_status s = paged_batch(c, fn, cache, &p.b);
     if (s != REKV_OK) return s;
-    const rekv::PagedPlan plan = paged_plan(c, cache->n_tokens, cache->n_seqs, max_kv, window, sinks, n_prefix);
+    rekv::PagedPlan plan;
+    s = paged_plan(c, fn, cache->n_tokens, cache->n_seqs, max_kv, window, sinks, n_prefix, &plan);
+    if (s != REKV_OK) return s;
     if (plan.workspace_bytes > 0 && (!workspace || workspace_bytes < plan.workspace_bytes || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0))
         return fail(c, REKV_ERR_INVALID_ARG, "%s: needs a 256-byte aligned workspace of %lld bytes, got %lld", fn, (long long)plan.workspace_bytes,
                     workspace ? (long long)workspace_bytes : 0ll);
-    const int64_t jobs = ((int64_t)plan.prefix_blocks * plan.prefix_splits + (int64_t)plan.blocks * plan.splits) * c->shape.n_kv_heads;
-    if (jobs > 0x7FFFFFFF) return fail(c, REKV_ERR_UNSUPPORTED, "%s: grid of %lld workgroups", fn, (long long)jobs);
     s = on_device(c, fn);
     if (s != REKV_OK) return s;
     p.q = q; p.out = out;
@@ -918,8 +928,10 @@ rekv_status rekv_attention_paged_workspace(rekv_ctx* c, int32_t n_tokens, int32_
         n_prefix >= MOST_KEYS)
         return fail(c, REKV_ERR_INVALID_ARG, "rekv_attention_paged_workspace: n_tokens=%d n_seqs=%d sinks=%d n_prefix=%d", n_tokens, n_seqs, sinks,
                     n_prefix);
-    *bytes = paged_plan(c, n_tokens, n_seqs, max_kv, window, sinks, n_prefix).workspace_bytes;
-    return REKV_OK;
+    rekv::PagedPlan plan;
+    const rekv_status s = paged_plan(c, "rekv_attention_paged_workspace", n_tokens, n_seqs, max_kv, window, sinks, n_prefix, &plan);
+    if (s == REKV_OK) *bytes = plan.workspace_bytes;
+    return s;
 }
 
 rekv_status rekv_probe_copy(rekv_ctx* c, void* dst, const void* src, int64_t n_bytes, void* stream) {

@@ -67,6 +67,19 @@ def test_wrong_arguments_are_refused():
     assert torch.equal(kp.nan_to_num(), dev(b.k_pages, "bf16").nan_to_num())
 
 
+def test_launches_that_are_too_large_are_refused():
+    r = Rekv(64, 8, 128, 16)
+    for n_tokens, n_seqs, n_prefix in ((2, (1 << 24) - 1, 0), ((1 << 24) - 1, 1 << 23, 5000)):
+        need = rekv.c_int64(7)
+        assert r._lib.rekv_attention_paged_workspace(r._h, n_tokens, n_seqs, 5000, -1, 0, n_prefix, rekv.byref(need)) == 2     # not supported
+        assert need.value == 0 and b"parts of the batch" in r._lib.rekv_last_error(r._h)
+    many = torch.zeros((1, 1, 1 << 20, 64), dtype=torch.bfloat16, device="cuda:0")
+    with pytest.raises(RekvError, match="64 MiB"):
+        Rekv(1 << 20, 1 << 20, 64, 16).attention_paged(many[0], many, many, ints([0, 1]), ints([1]), ints([[0]]))
+    need = rekv.c_int64(7)
+    assert r._lib.rekv_attention_paged_workspace(r._h, 1 << 20, 1000, 5000, -1, 0, 0, rekv.byref(need)) == 0 and need.value == 0
+
+
 def test_arguments_beyond_32_bits_do_not_wrap():
     b, r, (q, kp, vp, start, kv, table) = small()
     want = r.attention_paged(q, kp, vp, start, kv, table)
