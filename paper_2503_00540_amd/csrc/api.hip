@@ -793,15 +793,16 @@ static rekv_status rotary_args(rekv_ctx* c, const char* fn, const rekv_rotary* i
     for (int i = 0; i < in->n_axes; ++i) left[i] = in->sections[i];
     for (int i = 0, a = 0; i < half; ++i) {
         while (left[a] == 0) a = (a + 1) % in->n_axes;
-        r->axis[i] = (uint8_t)a;
+        r->axes[i / 16] |= (uint32_t)a << (2 * (i % 16));
         --left[a];
         if (in->order == 1) a = (a + 1) % in->n_axes;
     }
     // the frequencies as powers of one ratio, in extended precision
     const long double ratio = powl((long double)in->base, -2.0L / d);
-    long double theta = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
+    long double step = 1.0L, theta = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
     if (in->inverse) theta = -theta;
-    for (int i = 0; i < half; ++i, theta *= ratio) r->turns[i] = (double)theta;
+    for (int i = 0; i < 8; ++i, step *= ratio) r->fine[i] = (double)step;
+    for (int i = 0; i * 8 < half; ++i, theta *= step) r->coarse[i] = (double)theta;
     r->n_axes = in->n_axes;
     r->interleaved = in->layout;
     return REKV_OK;

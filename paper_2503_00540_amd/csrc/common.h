@@ -192,11 +192,13 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
                           int64_t window, int64_t sinks, int64_t n_prefix);
 hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int dtype, void* workspace, hipStream_t stream);
 
-// Rotary positions of one call: turns per position and axis of every pair.
+// Rotary positions of one call: pair i turns by coarse[i / 8] * fine[i % 8] per position.  (As products these take a few words of the
+// launch's arguments; with the 128 doubles themselves a call took 1.1 us more to issue.)
 constexpr int MAX_PAIRS = 128, MAX_AXES = 4;
 struct Rotary {
-    double turns[MAX_PAIRS];            // base^(-2i / D) / (2 pi), negative for the inverse
-    uint8_t axis[MAX_PAIRS];
+    double coarse[MAX_PAIRS / 8];       // base^(-16j / D) / (2 pi), negative for the inverse
+    double fine[8];                     // base^(-2j / D)
+    uint32_t axes[MAX_PAIRS / 16];      // two bits a pair
     int32_t n_axes, interleaved;        // n_axes 0: no rotation
 };
 struct RotateArgs {

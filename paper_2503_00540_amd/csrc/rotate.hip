@@ -3,7 +3,7 @@
 //   (x_a, x_b) -> (x_a cos t - x_b sin t, x_a sin t + x_b cos t),  t = position[axis of the pair] * base^(-2i / D)
 //
 // Bound: HBM for many tokens (50,176 x 28 heads of 128 out of a fused projection 121 us = 5.95 TB/s, a plain copy 5.96; append of
-// 26,800 tokens at 28/4/128 with their queries 92 us = 5.4 TB/s), the launch and its round trips for few (64 users 5.4 us).  A unit of work is one 16-byte chunk of a head
+// 26,800 tokens at 28/4/128 with their queries 92 us = 5.4 TB/s), the launch and its round trips for few (64 users 4.8 us).  A unit of work is one 16-byte chunk of a head
 // vector and its partner half a vector on, which hold both members of their pairs in either layout.  A lane keeps one
 // chunk position of one token and walks that token's heads, so that its angles (formed in double precision, reduced to a
 // fraction of a turn) are worked out once for all of them.
@@ -17,8 +17,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 constexpr int WAVES = 4;
-// Few tokens: their heads are divided until there are so many wavefronts (64 tokens of 64/8/128 with keys and values 6.5 us with four a
-// token, 5.4 with ten).
+// Few tokens: their heads are divided until there are so many wavefronts (64 tokens of 64/8/128 with keys and values 1.1 us less with ten a
+// token than with four, of 4.8).
 constexpr int FILL_WAVES = 4096;
 // At most so many wavefronts; the tokens beyond are walked.  Rotation of 50,176 x 28 heads of 128 (us): 128 with 8,192, 123 with 20,480, 121 with
 // 40,960, 153 with one per token; append of 24 streams' 26,800 tokens at 28/4/128: 93.3, 92.6, 94.5, 108.
@@ -71,11 +71,13 @@ __global__ __launch_bounds__(WAVES * 64) void rotate_kernel(RotateArgs a, int pa
     uint32_t axes = 0;                           // two bits a pair
     if (turn) {
 #pragma unroll
-        for (int e = 0; e < EPC; ++e) {
-            // pair e of this lane's two chunks: element e of both, or neighbours, the first half of them in the first chunk
-            const int i = a.r.interleaved ? (e >= EPC / 2 ? half / 2 : 0) + c * (EPC / 2) + e % (EPC / 2) : c * EPC + e;
-            turns[e] = a.r.turns[i];
-            axes |= (uint32_t)a.r.axis[i] << (2 * e);
+        for (int e = 0; e < EPC; e += 2) {
+            // pairs e and e + 1 of this lane's two chunks: elements of both, or neighbours, the first half of them in the first chunk; i is even
+            const uint32_t i = a.r.interleaved ? (e >= EPC / 2 ? half / 2 : 0) + c * (EPC / 2) + e % (EPC / 2) : c * EPC + e;
+            const double coarse = a.r.coarse[i / 8];
+            turns[e] = coarse * a.r.fine[i % 8];
+            turns[e + 1] = coarse * a.r.fine[i % 8 + 1];
+            axes |= (a.r.axes[i / 16] >> (2 * (i % 16)) & 15u) << (2 * e);
         }
     }
     const int last = base + per_wave - 1;        // of the first heads; the wavefront's last ones are a multiple of step on
