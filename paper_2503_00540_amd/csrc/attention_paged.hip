@@ -960,15 +960,20 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     PagedPlan plan;
     const int64_t keys = window < 0 || window + sinks > max_kv ? max_kv : window + sinks;
     // Blocks of 32 rows start and end sooner but fetch every tile four times as often: they take the sequences' own keys where few rows of
-    // a sequence share them, and where there is little to do in all: up to SMALL tiles of 128 rows per place (causal ones half).  28/4/128 and 14/2/64, as
-    // blocks of 128 and of 32 rows (us): a prompt of 196 tokens 13.8 and 8.6, 16 tokens over 3,000 17.8 and 14.1, a prompt of 1,000 34.7
-    // and 28.5, a live frame over 3,136 at 14/2/64 22.1 and 16.8; the other way 4 x 8 tokens over 8,000 18.7 and 20.4 (7.8 tiles a place),
-    // 32 x 16 over 3,000 42 and 58 (23), 4 live frames of 64/8/128 53 and 64 (23).
-    constexpr int64_t SMALL = 7;
+    // a sequence share them, and where the chip holds them in two rounds and has no more than SMALL tiles of 128 rows per place to do (causal
+    // ones half).  Blocks of 128 and of 32 rows at 28/4/128 (us): a prompt of 196 tokens 13.8 and 8.6, of 1,000 28 and 16, a live frame over
+    // 3,136 at 14/2/64 22.1 and 16.8, 8 x 60 tokens over 3,000 37 and 26; the other way 32 x 16 over 3,000 36 and 44 (23 tiles a place), 8
+    // x 160 through a window of 3,200 51 and 70 (26), in more than two rounds a prompt of 2,000 at 64/8/128 48 and 79, 80 x 50 tokens over 400 39 and 46.
+    // In the second round they need something to do: of 30 x 60 tokens over nothing 16 and 20, over 400 37 and 28.  On 250 random batches the
+    // choice takes 1.007 of the better time, one by tiles alone 1.054.  Beside a prefix, which larger batches have computed for all at once,
+    // SMALL is 7.
+    const int64_t SMALL = n_prefix > 0 ? 7 : 20;
     const int64_t row_blocks = up(all_rows, BM) > n_seqs ? up(all_rows, BM) : n_seqs;
+    const int64_t key_jobs = (up(all_rows, WM) > n_seqs ? up(all_rows, WM) : n_seqs) * n_kv_heads;
     const bool lone = all_rows <= n_seqs * WM;
     const int64_t causal = n_tokens / n_seqs < keys ? n_tokens / n_seqs : keys;
-    const bool small = row_blocks * n_kv_heads * up(keys + n_prefix - causal / 2, BN) <= SMALL * PLACES;
+    const bool rounds = key_jobs <= PLACES || (key_jobs <= 2 * PLACES && (head_dim < 128 || keys + n_prefix > 4 * BN));
+    const bool small = rounds && row_blocks * n_kv_heads * up(keys + n_prefix - causal / 2, BN) <= SMALL * PLACES;
     const bool few = bf16 && (lone || small);
 
     // Blocks of 128 rows in `jobs` times n workgroups over `tiles` tiles, in us: rounds of workgroups, each of about 8 us and tau a tile; and
@@ -1015,11 +1020,27 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
     const int64_t places = bf16 ? PLACES : 1024, busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
     const int64_t tiles = up(together ? keys : keys + n_prefix, BN);
-    // As many splits as fill the chip, each of two tiles a wavefront at least (a user's window of 15,000 tokens at 28/4/128 takes 16.7 us so,
-    // 18.7 with one, 17.5 with three).
+    // At most as many splits as fill the chip, each of two tiles a wavefront at least (a user's window of 15,000 tokens at 28/4/128 takes 16.7 us
+    // so, 18.7 with one, 17.5 with three).
     plan.min_tiles = few ? 8 : 4;
     int64_t s = places / (busy * n_kv_heads);
     if (s > up(tiles, plan.min_tiles)) s = up(tiles, plan.min_tiles);
+    if (few) {
+        // Of these, what an estimate says: a wavefront's tiles, 1.4 times as long with two workgroups on a CU, against the joining launch and
+        // the partial results (28/4/128, unsplit and filling the chip, us: a user's 450 tokens 9.2 and 9.8, 700 10.8 and 9.8, 2,000 19.0 and
+        // 10.7; 300 tokens over 1,400 20.1 and 22.5; 8 x 60 over 1,000 18.7 and 26.6).
+        double best = 1e30;
+        int64_t best_n = 1;
+        for (int64_t n = 1; n == 1 || n <= s; ++n) {
+            const double step = (head_dim == 128 ? 1.0 : 0.6) * (2 * busy * n_kv_heads * n > PLACES ? 1.4 : 1.0);
+            const double us = (double)tiles / (double)(WAVES * n) * step + (n > 1 ? (together ? 0.0 : 3.0) + (double)n * slot_us : 0.0);
+            if (us < best) {
+                best = us;
+                best_n = n;
+            }
+        }
+        s = best_n;
+    }
     // Where lone rows all but fill it, their lengths differ: pieces of one size, LONG tiles, spread the longer ones (64 users of 1 to 8,192
     // tokens at 64/8/128: 221 us whole, 207, 199, 199, 205 in pieces of 96, 64, 48, 32).
     constexpr int64_t LONG = 64, MOST_PIECES = 64;

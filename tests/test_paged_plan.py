@@ -46,7 +46,8 @@ def test_partial_results_of_many_rows_stay_few():
 @pytest.mark.parametrize("heads,tokens,seqs,kv,window,how", [
     (H72, 64, 64, 8192, -1, STREAMED), (H7, 1, 1, 50000, 15000, STREAMED),          # decode steps
     (H7, 196, 1, 196, -1, KEYS), (H7, 1000, 1, 1000, -1, KEYS), (H7, 16, 1, 3016, -1, KEYS), (H05, 196, 1, 12196, 3136, KEYS),
-    (H7, 8192, 1, 8192, -1, ROWS), (H72, 288, 4, 12144, 2304, ROWS), (H7, 610, 8, 12196, 3136, ROWS), (H7, 32, 4, 8008, -1, ROWS)])
+    (H7, 240, 8, 3060, -1, KEYS), (H7, 8192, 1, 8192, -1, ROWS), (H72, 2000, 1, 2000, -1, ROWS), (H72, 576, 4, 12144, 2304, ROWS),
+    (H7, 610, 8, 12196, 3136, ROWS), (H7, 270, 32, 3016, -1, ROWS), (H7, 900, 30, 60, -1, ROWS), (H7, 900, 30, 460, -1, KEYS)])
 def test_which_blocks_take_a_launch(heads, tokens, seqs, kv, window, how):
     assert plan(heads, tokens, seqs, kv, window)["how"] == how
 
