@@ -629,8 +629,8 @@ __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, co
     }
 }
 
-// ROW_BLOCKS: all by blocks of 128 rows.  KEY_BLOCKS, STREAMED: the sequences' own keys by blocks of 32 rows, a prefix shared by the
-// batch still by blocks of 128 (42 rows over 3,136 prefix tokens take 11.1 us so, 10.8 to 11.6 by blocks of 32).
+// ROW_BLOCKS: all by blocks of 128 rows.  KEY_BLOCKS, STREAMED: the sequences' own keys by blocks of 32 rows, a prefix computed
+// for the batch at once still by blocks of 128 (42 rows over 3,136 tokens take 11.1 us so, 10.8 to 11.6 by blocks of 32).
 template <int D, bool TWO_PAGES, int HOW>
 __global__ __launch_bounds__(THREADS, 2) void attn_paged_kernel(PagedArgs a) {
     constexpr bool FEW = HOW != ROW_BLOCKS;
@@ -983,15 +983,38 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     // blocks that ragged sequences fill, about; uneven over the XCDs
     const double own_jobs = (n_seqs == 1 ? (double)row_blocks : 1.15 * ((double)all_rows / BM + 0.5 * (double)n_seqs)) * (double)n_kv_heads;
 
+    // Blocks of 32 rows: in how many splits, of at most so many as fill the chip and two tiles a wavefront at least (a user's window of
+    // 15,000 tokens at 28/4/128 takes 16.7 us so, 18.7 with one, 17.5 with three), and in about how many us.  A round of workgroups takes 7
+    // and a wavefront's tiles, 1.4 times as long with two workgroups on a CU, or what its blocks' reads of a prefix take from the caches at 10
+    // TB/s; splits take the joining launch, if nothing else does, and the partial results (28/4/128, unsplit and filling the chip, us: a user's 450 tokens 9.2 and 9.8, 700 10.8 and 9.8, 2,000 19.0 and 10.7; 300
+    // tokens over 1,400 20.1 and 22.5; 8 x 60 over 1,000 18.7 and 26.6).
+    constexpr int64_t FEW_TILES = 2 * WAVES;
+    const double few_jobs = (double)key_jobs;
+    auto few_us = [&](int64_t tiles, int64_t prefix, bool joined, int64_t* splits) {
+        double best = 1e30;
+        const double reads = few_jobs * (double)(prefix * head_dim * 4) / 10e6;
+        for (int64_t n = 1; n == 1 || (n * key_jobs <= PLACES && n <= up(tiles, FEW_TILES)); ++n) {
+            const double step = (head_dim == 128 ? 1.0 : 0.6) * (2.0 * few_jobs * (double)n > PLACES ? 1.4 : 1.0);
+            const double in_turn = ceil(few_jobs * (double)n / PLACES), walk = in_turn * (double)tiles / (double)(WAVES * n) * step;
+            const double us = in_turn * 7.0 + (walk > reads ? walk : reads) + (n > 1 ? (joined ? 0.0 : 3.0) + (double)n * slot_us : 0.0);
+            if (us < best) {
+                best = us;
+                *splits = n;
+            }
+        }
+        return best;
+    };
+    int64_t few_splits = 1;
+
     // A prefix is computed for the batch at once, by full blocks of all sequences' rows whose results are joined with the own keys', or
     // walked by each sequence's own blocks.  Measured, walked and at once (us, 28/4/128, a prefix of 4,608): 64 sequences of 12 tokens 119
     // and 77, of 24 211 and 132, of 32 228 and 158, of 48 260 and 249, of 64 280 and 305, 24 of 40 128 and 86, 16 of 12 45 and 36.  The estimate is off
     // by a tenth where the two are alike: of these it takes the slower one at 48 and at 64 tokens.
     plan.prefix_blocks = plan.prefix_splits = 0;
     plan.min_prefix_tiles = 4;
-    bool together = n_prefix > 0 && (bf16 ? lone : all_rows < n_seqs * (F32_ROWS / 2));
+    bool together = n_prefix > 0 && !bf16 && all_rows < n_seqs * (F32_ROWS / 2);
     const int64_t prefix_rows = bf16 ? BM : F32_ROWS, prefix_tiles = up(n_prefix, BN);
-    if (n_prefix > 0 && (together || (bf16 && !small))) {
+    if (n_prefix > 0 && (together || (bf16 && (lone || !small)))) {
         plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
         plan.prefix_splits = 1;
         const double jobs = (double)plan.prefix_blocks * (double)n_kv_heads;
@@ -1007,39 +1030,29 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
                 plan.prefix_splits = (int32_t)n;
             }
         }
-        if (!together) {
+        if (bf16 && lone) {
+            // (of 125 random batches 1.015 of the better time; all at once 1.26, all walked 1.08)
+            const double own = few_us(up(keys, BN), 0, true, &few_splits);
+            together = (best > own ? best : own) + slot_us + 1.0 < few_us(up(keys + n_prefix, BN), n_prefix, false, &few_splits);
+        } else if (!together) {
             const int64_t s = PLACES / (row_blocks * n_kv_heads), tiles = up(keys + n_prefix, BN);
             const double walked = rows_us(own_jobs, tiles, s > 1 ? s : 1) + (s > 1 ? (double)s * slot_us + 4.0 : 0.0);
             together = best + rows_us(own_jobs, up(keys, BN), 1) + slot_us + 4.0 < walked;
-            if (!together) plan.prefix_blocks = plan.prefix_splits = 0;
         }
+        if (!together) plan.prefix_blocks = plan.prefix_splits = 0;
     }
 
-    plan.how = !few ? ROW_BLOCKS : lone ? STREAMED : KEY_BLOCKS;
+    plan.how = !few ? ROW_BLOCKS : lone && (together || n_prefix == 0 || n_seqs == 1) ? STREAMED : KEY_BLOCKS;     // (a walked prefix is shared)
     plan.rows = !bf16 ? F32_ROWS : few ? WM : BM;
     plan.blocks = (int32_t)(all_rows / plan.rows + n_seqs);
     const int64_t places = bf16 ? PLACES : 1024, busy = up(all_rows, plan.rows) > n_seqs ? up(all_rows, plan.rows) : n_seqs;
     const int64_t tiles = up(together ? keys : keys + n_prefix, BN);
-    // At most as many splits as fill the chip, each of two tiles a wavefront at least (a user's window of 15,000 tokens at 28/4/128 takes 16.7 us
-    // so, 18.7 with one, 17.5 with three).
-    plan.min_tiles = few ? 8 : 4;
+    plan.min_tiles = few ? FEW_TILES : 4;
     int64_t s = places / (busy * n_kv_heads);
     if (s > up(tiles, plan.min_tiles)) s = up(tiles, plan.min_tiles);
     if (few) {
-        // Of these, what an estimate says: a wavefront's tiles, 1.4 times as long with two workgroups on a CU, against the joining launch and
-        // the partial results (28/4/128, unsplit and filling the chip, us: a user's 450 tokens 9.2 and 9.8, 700 10.8 and 9.8, 2,000 19.0 and
-        // 10.7; 300 tokens over 1,400 20.1 and 22.5; 8 x 60 over 1,000 18.7 and 26.6).
-        double best = 1e30;
-        int64_t best_n = 1;
-        for (int64_t n = 1; n == 1 || n <= s; ++n) {
-            const double step = (head_dim == 128 ? 1.0 : 0.6) * (2 * busy * n_kv_heads * n > PLACES ? 1.4 : 1.0);
-            const double us = (double)tiles / (double)(WAVES * n) * step + (n > 1 ? (together ? 0.0 : 3.0) + (double)n * slot_us : 0.0);
-            if (us < best) {
-                best = us;
-                best_n = n;
-            }
-        }
-        s = best_n;
+        few_us(tiles, together ? 0 : n_prefix, together, &few_splits);
+        s = few_splits;
     }
     // Where lone rows all but fill it, their lengths differ: pieces of one size, LONG tiles, spread the longer ones (64 users of 1 to 8,192
     // tokens at 64/8/128: 221 us whole, 207, 199, 199, 205 in pieces of 96, 64, 48, 32).

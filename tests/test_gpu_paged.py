@@ -91,6 +91,13 @@ def test_many_sequences(heads):
         attend(Batch(new, kv, 16, *heads[:3], "bf16", pad=5))
 
 
+@pytest.mark.parametrize("page", [16, 20, 64])
+def test_many_users_single_tokens_after_a_long_prefix(page):
+    """Long enough to be computed for the batch at once; a short one is walked by every user's block."""
+    for prefix in (6000, 100):
+        attend(Batch([1] * 40, [1 + 7 * i % 40 for i in range(40)], page, 28, 4, 128, n_prefix=prefix, pad=2), every=1 if prefix < 1000 else 9)
+
+
 def test_negative_indexes_and_lengths_beyond_the_table():
     # more new tokens than tokens in all: the first ones have no index, see nothing and get zeros
     for heads in (HEADS[0], HEADS[3]):

@@ -53,7 +53,7 @@ def test_which_blocks_take_a_launch(heads, tokens, seqs, kv, window, how):
 
 
 @pytest.mark.parametrize("tokens,seqs,own,prefix,at_once", [
-    (64, 64, 400, 25088, True), (6, 6, 91, 3136, True), (64 * 12, 64, 12, 4608, True), (64 * 32, 64, 32, 4608, True), (24 * 40, 24, 40, 4608, True),
+    (64, 64, 400, 25088, True), (6, 6, 91, 3136, True), (40, 40, 40, 6000, True), (64, 64, 400, 100, False), (1, 1, 4, 5216, False), (64 * 12, 64, 12, 4608, True), (64 * 32, 64, 32, 4608, True), (24 * 40, 24, 40, 4608, True),
     (64 * 512, 64, 512, 4608, False), (4 * 8, 4, 8, 4608, False)])
 def test_which_prefixes_are_computed_at_once(tokens, seqs, own, prefix, at_once):
     assert (plan(H7, tokens, seqs, own, prefix=prefix)["prefix_blocks"] > 0) == at_once
@@ -65,3 +65,9 @@ def test_splits_fill_the_chip_and_no_more():
     p = plan(H7, 64, 64, 400, prefix=25088)
     assert p["prefix_blocks"] == 4 and p["prefix_splits"] == 24                      # beside 256 workgroups of own keys
     assert plan(H72, 64, 64, 8192)["splits"] == 4 and plan(H72, 64, 64, 10 ** 9)["splits"] == 64
+
+
+def test_a_short_prefix_takes_one_launch():
+    for heads, tokens, own, prefix in ((H7, 64, 40, 100), (H72, 64, 13, 157), (H05, 20, 1, 15), ((8, 8, 64), 5, 9, 4)):
+        p = plan(heads, tokens, tokens, own, prefix=prefix)
+        assert p["how"] == KEYS and p["splits"] == 1 and p["bytes"] == 0
