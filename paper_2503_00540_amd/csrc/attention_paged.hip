@@ -1012,7 +1012,10 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     // by a tenth where the two are alike: of these it takes the slower one at 48 and at 64 tokens.
     plan.prefix_blocks = plan.prefix_splits = 0;
     plan.min_prefix_tiles = 4;
-    bool together = n_prefix > 0 && !bf16 && all_rows < n_seqs * (F32_ROWS / 2);
+    // (fp32: lone rows walk a prefix of up to F32_SHORT tiles, and up to F32_WHOLE tiles are not split.  30 users' tokens after five tiles at
+    // 14/2/64 take 10.5 us at once, 9.5 walked in two splits, 8.0 in one; after 13 tiles 11.1, 11.1 and 13.1; after 32 11.1 and 15.2.)
+    constexpr int64_t F32_SHORT = 16, F32_WHOLE = 8;
+    bool together = !bf16 && all_rows < n_seqs * (F32_ROWS / 2) && n_prefix > F32_SHORT * BN;
     const int64_t prefix_rows = bf16 ? BM : F32_ROWS, prefix_tiles = up(n_prefix, BN);
     if (n_prefix > 0 && (together || (bf16 && (lone || !small)))) {
         plan.prefix_blocks = (int32_t)up(all_rows, prefix_rows);
@@ -1050,6 +1053,7 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     plan.min_tiles = few ? FEW_TILES : 4;
     int64_t s = places / (busy * n_kv_heads);
     if (s > up(tiles, plan.min_tiles)) s = up(tiles, plan.min_tiles);
+    if (!bf16 && tiles <= F32_WHOLE) s = 1;
     if (few) {
         few_us(tiles, together ? 0 : n_prefix, together, &few_splits);
         s = few_splits;
