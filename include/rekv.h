@@ -467,7 +467,7 @@ rekv_status rekv_attention_paged(rekv_ctx* ctx, const rekv_paged* cache, const v
                                  int64_t workspace_bytes, void* stream);
 
 /*
- * The same for a batch that shares a long prefix, computed once for all its rows: every new token sees
+ * The same for a batch that shares a prefix (a long one is computed once for all its rows): every new token sees
  * all n_prefix >= 1 tokens of the prefix and, causally, its own sequence's tokens.  kv_len, the
  * indexes and page_table count the own tokens only.
  *   prefix_pages  device int32 [ceil(n_prefix / page_size)], pages of the same cache

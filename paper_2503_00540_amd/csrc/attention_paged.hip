@@ -8,8 +8,8 @@
 // or between a prefix and the row's own keys, each part leaves (m, sum, O) in fp32 and a second launch joins them.
 //
 // Rows are stacked as in attention_bf16.hip, the G query heads of a KV head token by token, so a K/V tile in LDS
-// serves them all; a prefix shared by the batch is walked by blocks of all sequences' rows, so that one user's few rows do not
-// read it for themselves.  Operand layouts, the four LDS stages per tensor and the order of a step are those of attention_bf16.hip.
+// serves them all; a long prefix shared by the batch is walked by blocks of all sequences' rows, so that one user's few rows do
+// not read it for themselves (a short one they do, which saves the second launch).  Operand layouts, the four LDS stages per tensor and the order of a step are those of attention_bf16.hip.
 // What differs is where tiles come from: 32 keys lie in one or two pages, and the places of 64 tiles are worked out at once.
 //
 // What bounds it (28/4/128, pages of 64 to 256 unless said).  Long prompts: the matrix cores at the clock the chip grants them,

@@ -679,7 +679,7 @@ class Rekv:
     def attention_shared_prefix(self, q, k_pages, v_pages, prefix_pages, n_prefix: int, token_start, kv_len, page_table,
                                 max_kv: int | None = None, out=None):
         """rekv_attention_shared_prefix: as attention_paged without a window, where every token also sees the n_prefix tokens in
-        prefix_pages (int32), computed once for the batch; kv_len and page_table count the own tokens only."""
+        prefix_pages (int32), a long prefix computed once for the batch; kv_len and page_table count the own tokens only."""
         done = self._fast.attention_shared_prefix(q, k_pages, v_pages, prefix_pages, n_prefix, token_start, kv_len, page_table, max_kv, out)
         if done is not None:
             return done
