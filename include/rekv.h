@@ -425,7 +425,8 @@ typedef struct {
  * Rotates n_tokens x n_heads head vectors.
  *   x, out     [n_tokens, n_heads, D], tokens x_stride and out_stride elements apart (at least
  *              n_heads * D, multiples of 16 bytes); out may be x itself with the same stride
- *   positions  device int32 [n_axes, n_tokens], axes positions_stride (at least n_tokens) apart
+ *   positions  device int32 [n_axes, n_tokens], axes positions_stride (at least n_tokens) apart; 0: one row
+ *              [n_tokens] for all axes, as text has it
  */
 rekv_status rekv_rotate(rekv_ctx* ctx, const rekv_rotary* rotary, const void* x, int64_t x_stride,
                         int32_t n_tokens, int32_t n_heads, const int32_t* positions, int64_t positions_stride,
@@ -437,8 +438,8 @@ rekv_status rekv_rotate(rekv_ctx* ctx, const rekv_rotary* rotary, const void* x,
  *   k, v       [n_tokens, Hkv, D], tokens k_stride and v_stride elements apart
  *   q, q_out   [n_tokens, Hq, D], tokens q_stride apart, q_out dense; both NULL: no queries; q_out may be q
  *   rotary     NULL: keys (and queries) are taken as they are
- *   positions  device int32 [n_axes, n_tokens]; NULL: a token's position is its index in its
- *              sequence, on every axis
+ *   positions  device int32 [n_axes, n_tokens], positions_stride as above; NULL: a token's position is its
+ *              index in its sequence, on every axis
  * kv_len counts the new tokens.  Tokens whose index lies outside the table's max_pages, or whose page
  * is outside [0, n_pages), are not written; no two tokens may have the same place.  Rows of q_out behind the last
  * sequence stay as they were.

@@ -813,7 +813,7 @@ rekv_status rekv_rotate(rekv_ctx* c, const rekv_rotary* rotary, const void* x, i
                         void* stream) {
     if (!c) return REKV_ERR_INVALID_ARG;
     if (!rotary || !x || !positions || !out) return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: null pointer");
-    if (n_tokens <= 0 || n_heads <= 0 || positions_stride < n_tokens)
+    if (n_tokens <= 0 || n_heads <= 0 || (positions_stride < n_tokens && positions_stride != 0))
         return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: n_tokens=%d n_heads=%d positions_stride=%lld", n_tokens, n_heads, (long long)positions_stride);
     if (n_tokens >= (1 << 30)) return fail(c, REKV_ERR_UNSUPPORTED, "rekv_rotate: %d tokens are too many", n_tokens);
     rekv::RotateArgs a;
@@ -845,7 +845,7 @@ rekv_status rekv_append_kv(rekv_ctx* c, const rekv_paged* cache, const rekv_rota
     rekv_status s = paged_batch(c, "rekv_append_kv", cache, &a.b);
     if (s == REKV_OK) s = rotary_args(c, "rekv_append_kv", rotary, &a.r);
     if (s != REKV_OK) return s;
-    if (positions && positions_stride < cache->n_tokens)
+    if (positions && positions_stride < cache->n_tokens && positions_stride != 0)
         return fail(c, REKV_ERR_INVALID_ARG, "rekv_append_kv: positions_stride=%lld for %d tokens", (long long)positions_stride, cache->n_tokens);
     const int64_t d = c->shape.head_dim, kv_row = c->shape.n_kv_heads * d, q_row = c->shape.n_q_heads * d, lane = 16 / (int64_t)elem_size(c);
     if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || k_stride < kv_row || v_stride < kv_row || (q && q_stride < q_row) ||

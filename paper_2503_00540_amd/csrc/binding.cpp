@@ -510,7 +510,7 @@ struct Rotation {
     }
 };
 
-// int32 [n_axes, n_tokens], or [n_tokens] for one axis; the elements between axes.
+// int32 [n_axes, n_tokens], or [n_tokens] for one axis; the elements between axes (0: expanded, the same for all).
 const Tensor* positions_of(Args& g, PyObject* o, int64_t n_tokens, int64_t n_axes, int64_t* stride) {
     const Tensor* t = g.tensor(o);
     if (!t) return nullptr;

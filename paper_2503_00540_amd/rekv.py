@@ -555,7 +555,7 @@ class Rekv:
         return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
 
     def _positions(self, positions, n_tokens, n_axes):
-        """[n_axes, n_tokens] (or [n_tokens] for one axis) int32; returns the elements between axes."""
+        """[n_axes, n_tokens] (or [n_tokens] for one axis) int32; returns the elements between axes (0: expanded, the same for all)."""
         if positions.dim() == 1 and n_axes == 1:
             positions = positions[None]
         if positions.dim() != 2 or positions.dtype != torch.int32 or tuple(positions.shape) != (n_axes, n_tokens) or positions.stride(1) != 1:
@@ -635,7 +635,7 @@ class Rekv:
         self._check(self._lib.rekv_append_kv(
             self._h, byref(cache), byref(rotary) if rotate else None, k.data_ptr(), k_stride, v.data_ptr(), v_stride,
             q.data_ptr() if q is not None else None, q_stride, q_out.data_ptr() if q is not None else None,
-            positions.data_ptr() if p_stride else None, p_stride, _stream()))
+            positions.data_ptr() if positions is not None else None, p_stride, _stream()))
         return q_out
 
     def _attention_paged(self, q, cache, n_prefix, prefix_pages, max_kv, window, sinks, out):

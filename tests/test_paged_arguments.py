@@ -1,0 +1,56 @@
+"""What the Python methods of the paged-cache calls hand to the C calls, without a GPU: a stand-in for the library records it."""
+
+import pytest
+import torch
+
+from paper_2503_00540_amd import rekv
+
+
+class Recorded(rekv.Rekv):
+    """The Python methods on host tensors, before a library that notes its arguments and succeeds."""
+
+    def __init__(self, monkeypatch):
+        monkeypatch.setattr(rekv, "_stream", lambda: 0)
+        self.n_q_heads, self.n_kv_heads, self.head_dim, self.tokens_per_frame, self.torch_dtype = 4, 2, 64, 16, torch.bfloat16
+        self._h, self._fast, self._lib, self.calls = None, rekv._NoNative(), self, []
+
+    def __getattr__(self, name):
+        if not name.startswith("rekv_"):
+            raise AttributeError(name)
+
+        def call(*args):
+            self.calls.append((name, args))
+            return 0
+        return call
+
+    def _here(self, **tensors):
+        pass
+
+    def _dev(self, t, dtype=None, last=None, name="tensor"):
+        return t.data_ptr()
+
+
+def bf(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def i32(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+@pytest.fixture
+def r(monkeypatch):
+    return Recorded(monkeypatch)
+
+
+@pytest.mark.parametrize("n", [1, 5])
+def test_one_row_of_positions_expanded_over_the_axes_is_handed_on(r, n):
+    row = i32(n)
+    for pos, stride in ((row.expand(3, -1), 0), (row.repeat(3, 1), n), (i32(3, n + 2)[:, :n], n + 2)):
+        r.append_kv(bf(n, 2, 64), bf(n, 2, 64), bf(5, 16, 2, 64), bf(5, 16, 2, 64), i32(2), i32(1), i32(1, 3), positions=pos, sections=[8, 12, 12])
+        r.rotate(bf(n, 4, 64), pos, sections=[8, 12, 12])
+        (_, append), (_, rotate) = r.calls[-2:]
+        assert append[-3] == pos.data_ptr() and append[-2] == stride
+        assert rotate[6] == pos.data_ptr() and rotate[7] == stride
+    r.append_kv(bf(n, 2, 64), bf(n, 2, 64), bf(5, 16, 2, 64), bf(5, 16, 2, 64), i32(2), i32(1), i32(1, 3))
+    assert r.calls[-1][1][-3] is None
