@@ -113,6 +113,8 @@ struct Args {
         return ok ? static_cast<const int32_t*>(t->data_ptr()) : nullptr;
     }
     static bool fits(int64_t v) { return v == (int32_t)v; }
+    // neighbours of the last dimension; a single one has none, whatever stride a view left it
+    static bool side_by_side(const Tensor* t) { return t->size(-1) <= 1 || t->stride(-1) == 1; }
 };
 
 void* ptr(const Tensor& t) { return t.data_ptr(); }
@@ -516,7 +518,7 @@ const Tensor* positions_of(Args& g, PyObject* o, int64_t n_tokens, int64_t n_axe
     if (!t) return nullptr;
     const bool flat = t->dim() == 1 && n_axes == 1;
     g.need(g.here(t) && t->scalar_type() == at::kInt && (flat || (t->dim() == 2 && t->size(0) == n_axes)));
-    g.need(g.ok && t->size(-1) == n_tokens && t->stride(-1) == 1);
+    g.need(g.ok && t->size(-1) == n_tokens && Args::side_by_side(t));
     if (!g.ok) return nullptr;
     *stride = n_axes > 1 ? t->stride(0) : n_tokens;
     return t;
@@ -530,7 +532,7 @@ struct Batch {
         if (!g.ok) return;
         g.need(g.here(k) && g.here(v) && v->sizes() == k->sizes() && Args::fits(k->size(0)) && Args::fits(k->size(1)) && Args::fits(n_tokens));
         for (int i = 0; i < 3; ++i)
-            g.need(g.ok && g.here(t[i]) && t[i]->scalar_type() == at::kInt && t[i]->dim() == (i == 2 ? 2 : 1) && t[i]->stride(-1) == 1);
+            g.need(g.ok && g.here(t[i]) && t[i]->scalar_type() == at::kInt && t[i]->dim() == (i == 2 ? 2 : 1) && Args::side_by_side(t[i]));
         if (!g.ok) return;
         const int64_t n = t[1]->size(0);
         g.need(Args::fits(n) && t[0]->size(0) == n + 1 && t[2]->size(0) == n && Args::fits(t[2]->size(1)));

@@ -158,6 +158,11 @@ else:
         return torch.cuda.current_stream().cuda_stream
 
 
+def _side_by_side(t: torch.Tensor) -> bool:
+    """Neighbours of the last dimension; a single one has none, whatever stride a view left it."""
+    return t.shape[-1] <= 1 or t.stride(-1) == 1
+
+
 class Rekv:
     """One layer shape's context.  Methods mirror the C entry points one to one."""
 
@@ -558,7 +563,7 @@ class Rekv:
         """[n_axes, n_tokens] (or [n_tokens] for one axis) int32; returns the elements between axes (0: expanded, the same for all)."""
         if positions.dim() == 1 and n_axes == 1:
             positions = positions[None]
-        if positions.dim() != 2 or positions.dtype != torch.int32 or tuple(positions.shape) != (n_axes, n_tokens) or positions.stride(1) != 1:
+        if positions.dim() != 2 or positions.dtype != torch.int32 or tuple(positions.shape) != (n_axes, n_tokens) or not _side_by_side(positions):
             raise ValueError(f"positions must be int32 [{n_axes}, {n_tokens}] with a token's neighbours side by side, got {tuple(positions.shape)} "
                              f"of {positions.dtype}")
         return positions.stride(0) if n_axes > 1 else n_tokens
@@ -576,7 +581,7 @@ class Rekv:
         if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
             raise ValueError("k_pages / v_pages must both be [n_pages, page_size, Hkv, D]")
         for t, dims, name in ((token_start, 1, "token_start"), (kv_len, 1, "kv_len"), (page_table, 2, "page_table")):
-            if t.dim() != dims or t.dtype != torch.int32 or t.stride(-1) != 1:
+            if t.dim() != dims or t.dtype != torch.int32 or not _side_by_side(t):
                 raise ValueError(f"{name} must be int32 with {dims} dimension(s), neighbours side by side")
         n_seqs = kv_len.shape[0]
         if token_start.shape[0] != n_seqs + 1 or page_table.shape[0] != n_seqs:

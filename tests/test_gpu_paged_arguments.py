@@ -42,3 +42,21 @@ def test_positions_expanded_over_the_axes(dtype, new, kv):
             assert torch.equal(got, want_q) and torch.equal(a.nan_to_num(9.0), want_k.nan_to_num(9.0)), (half, base)
             assert torch.equal(c.nan_to_num(9.0), want_v.nan_to_num(9.0))
             assert torch.equal(r.rotate(q, row.expand(3, -1), base=base, **args), want), (half, base)
+
+
+def test_views_that_leave_one_element_with_a_stride():
+    """One token of one sequence whose positions, length and page number are cut out of larger tensors."""
+    b = Batch([1], [33], 64, 14, 2, 64)
+    r, (q, kp, vp, start, lens, table) = Rekv(14, 2, 64, 64), b.device()
+    k, v = (torch.randn((1, 2, 64), device="cuda:0").to(torch.bfloat16) for _ in range(2))
+    pos = ints([[7, 800, 31]])
+    cut_lens, cut_table = ints([[0, 33], [5, 6]])[:1, 1], table.T.as_strided((1, 1), (1, 9))
+    args = dict(sections=[8, 12, 12], q=q)
+    want_k = kp.clone()
+    want_q = r.append_kv(k, v, want_k, vp.clone(), start, lens, table, positions=pos.T.clone(memory_format=torch.contiguous_format), **args)
+    want = r.attention_paged(q, kp, vp, start, lens, table)
+    for half in halves(r):
+        a = kp.clone()
+        got = r.append_kv(k, v, a, vp.clone(), start, cut_lens, cut_table, positions=pos.T, **args)
+        assert torch.equal(got, want_q) and torch.equal(a.nan_to_num(9.0), want_k.nan_to_num(9.0)), half
+        assert torch.equal(r.attention_paged(q, kp, vp, start, cut_lens, cut_table), want), half

@@ -54,3 +54,15 @@ def test_one_row_of_positions_expanded_over_the_axes_is_handed_on(r, n):
         assert rotate[6] == pos.data_ptr() and rotate[7] == stride
     r.append_kv(bf(n, 2, 64), bf(n, 2, 64), bf(5, 16, 2, 64), bf(5, 16, 2, 64), i32(2), i32(1), i32(1, 3))
     assert r.calls[-1][1][-3] is None
+
+
+def test_a_single_element_has_no_neighbour(r):
+    """A view leaves a dimension of one element any stride, which contiguous() does not change either."""
+    pos = i32(1, 3).T
+    lens, table = i32(2, 7)[:1, 3], i32(1, 1).as_strided((1, 1), (1, 5))
+    assert pos.stride() == (1, 3) and pos.contiguous().stride(1) == 3 and lens.stride() == (7,)
+    r.append_kv(bf(1, 2, 64), bf(1, 2, 64), bf(5, 16, 2, 64), bf(5, 16, 2, 64), i32(2), lens, table, positions=pos, sections=[8, 12, 12])
+    assert r.calls[-1][1][-3] == pos.data_ptr() and r.calls[-1][1][-2] == 1
+    r.rotate(bf(1, 4, 64), pos, sections=[8, 12, 12])
+    with pytest.raises(ValueError, match="side by side"):
+        r.append_kv(bf(2, 2, 64), bf(2, 2, 64), bf(5, 16, 2, 64), bf(5, 16, 2, 64), i32(3), i32(2, 7)[:, 3], i32(2, 1))
