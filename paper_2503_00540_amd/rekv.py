@@ -163,6 +163,13 @@ def _side_by_side(t: torch.Tensor) -> bool:
     return t.shape[-1] <= 1 or t.stride(-1) == 1
 
 
+def _sizes(**sizes):
+    """What a 32-bit argument can hold: ctypes would wrap the others without a word."""
+    for name, n in sizes.items():
+        if n >= 1 << 31:
+            raise ValueError(f"{name}={n} must be below 2^31")
+
+
 class Rekv:
     """One layer shape's context.  Methods mirror the C entry points one to one."""
 
@@ -586,6 +593,7 @@ class Rekv:
         n_seqs = kv_len.shape[0]
         if token_start.shape[0] != n_seqs + 1 or page_table.shape[0] != n_seqs:
             raise ValueError("token_start must be [n_seqs + 1], kv_len [n_seqs], page_table [n_seqs, pages]")
+        _sizes(n_pages=k_pages.shape[0], page_size=k_pages.shape[1], n_seqs=n_seqs, n_tokens=n_tokens, max_pages=page_table.shape[1])
         return RekvPaged(self._dev(k_pages, last=kh, name="k_pages"), self._dev(v_pages, last=kh, name="v_pages"), token_start.data_ptr(),
                          kv_len.data_ptr(), page_table.data_ptr(), page_table.stride(0) if n_seqs > 1 else page_table.shape[1],
                          page_table.shape[1], k_pages.shape[0], k_pages.shape[1], n_seqs, n_tokens)
@@ -599,6 +607,7 @@ class Rekv:
             return done
         self._here(x=x, positions=positions, out=out)
         x_stride = self._tokens(x, None, "x")
+        _sizes(n_tokens=x.shape[0], n_heads=x.shape[1])
         rotary = self._rotary(sections, base, layout, order, inverse)
         p_stride = self._positions(positions, x.shape[0], rotary.n_axes)
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out

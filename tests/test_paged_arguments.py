@@ -66,3 +66,25 @@ def test_a_single_element_has_no_neighbour(r):
     r.rotate(bf(1, 4, 64), pos, sections=[8, 12, 12])
     with pytest.raises(ValueError, match="side by side"):
         r.append_kv(bf(2, 2, 64), bf(2, 2, 64), bf(5, 16, 2, 64), bf(5, 16, 2, 64), i32(3), i32(2, 7)[:, 3], i32(2, 1))
+
+
+def test_sizes_beyond_32_bits_are_refused(r):
+    """Of tensors without storage; a wrapped number of tokens or pages would serve a part of them and report success."""
+    def meta(*shape, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    big = (1 << 32) + 1
+    ok = dict(n=3, pages=5, page=16, seqs=1, table=3)
+    for name, size in ok.items():
+        a = dict(ok, **{name: big})
+        kp = meta(a["pages"], a["page"], 2, 64)
+        batch = (kp, kp, meta(a["seqs"] + 1, dtype=torch.int32), meta(a["seqs"], dtype=torch.int32), meta(a["seqs"], a["table"], dtype=torch.int32))
+        k, q = meta(a["n"], 2, 64), meta(a["n"], 4, 64)
+        for call in (lambda: r.append_kv(k, k, *batch), lambda: r.attention_paged(q, *batch),
+                     lambda: r.attention_shared_prefix(q, kp, kp, meta(2, dtype=torch.int32), 20, *batch[2:])):
+            with pytest.raises(ValueError, match="2.31"):
+                call()
+    for shape in ((big, 1, 64), (1, big, 64)):
+        with pytest.raises(ValueError, match="2.31"):
+            r.rotate(meta(*shape), meta(shape[0], dtype=torch.int32))
+    assert not r.calls
