@@ -422,7 +422,7 @@ typedef struct {
 } rekv_rotary;
 
 /*
- * Rotates n_tokens x n_heads head vectors.
+ * Rotates n_tokens x n_heads head vectors, either number below 2^30.
  *   x, out     [n_tokens, n_heads, D], tokens x_stride and out_stride elements apart (at least
  *              n_heads * D, multiples of 16 bytes); out may be x itself with the same stride
  *   positions  device int32 [n_axes, n_tokens], axes positions_stride (at least n_tokens) apart; 0: one row

@@ -815,7 +815,9 @@ rekv_status rekv_rotate(rekv_ctx* c, const rekv_rotary* rotary, const void* x, i
     if (!rotary || !x || !positions || !out) return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: null pointer");
     if (n_tokens <= 0 || n_heads <= 0 || (positions_stride < n_tokens && positions_stride != 0))
         return fail(c, REKV_ERR_INVALID_ARG, "rekv_rotate: n_tokens=%d n_heads=%d positions_stride=%lld", n_tokens, n_heads, (long long)positions_stride);
-    if (n_tokens >= (1 << 30)) return fail(c, REKV_ERR_UNSUPPORTED, "rekv_rotate: %d tokens are too many", n_tokens);
+    // (the kernel steps over heads by up to four times 64 in each of 4,096 wavefronts, in 32 bits)
+    if (n_tokens >= (1 << 30) || n_heads >= (1 << 30))
+        return fail(c, REKV_ERR_UNSUPPORTED, "rekv_rotate: %d tokens of %d heads are too many", n_tokens, n_heads);
     rekv::RotateArgs a;
     memset(&a, 0, sizeof(a));
     rekv_status s = rotary_args(c, "rekv_rotate", rotary, &a.r);
