@@ -477,7 +477,10 @@ rekv_status rekv_attention_shared_prefix(rekv_ctx* ctx, const rekv_paged* cache,
                                          const int32_t* prefix_pages, int32_t n_prefix, int32_t max_kv,
                                          void* out, void* workspace, int64_t workspace_bytes, void* stream);
 
-/* Workspace of the two calls above (n_prefix 0: rekv_attention_paged), which depends on sizes alone.  Host call. */
+/*
+ * Workspace of the two calls above, which depends on sizes alone.  Host call.  n_prefix 0: of rekv_attention_paged;
+ * otherwise of rekv_attention_shared_prefix, which has no window, so window and sinks are not looked at.
+ */
 rekv_status rekv_attention_paged_workspace(rekv_ctx* ctx, int32_t n_tokens, int32_t n_seqs, int32_t max_kv,
                                            int32_t window, int32_t sinks, int32_t n_prefix, int64_t* bytes);
 

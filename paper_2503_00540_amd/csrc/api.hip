@@ -871,6 +871,7 @@ constexpr int32_t MOST_KEYS = 1 << 30;       // no sequence is longer: a larger 
 // where the rows do not divide a workgroup.
 static rekv_status paged_plan(rekv_ctx* c, const char* fn, int64_t n_tokens, int64_t n_seqs, int32_t max_kv, int32_t window, int32_t sinks,
                               int64_t n_prefix, rekv::PagedPlan* plan) {
+    if (n_prefix > 0) window = -1, sinks = 0;     // as rekv_attention_shared_prefix has it, whatever a query names
     *plan = rekv::attn_paged_plan(c->shape.dtype, c->shape.n_q_heads, c->shape.n_kv_heads, c->shape.head_dim, n_tokens, n_seqs,
                                   max_kv < 1 ? 1 : max_kv < MOST_KEYS ? max_kv : MOST_KEYS, window < MOST_KEYS ? window : -1, sinks, n_prefix);
     const int64_t jobs = ((int64_t)plan->prefix_blocks * plan->prefix_splits + (int64_t)plan->blocks * plan->splits) * c->shape.n_kv_heads;

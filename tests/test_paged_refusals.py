@@ -32,3 +32,23 @@ def test_rotations_whose_heads_or_tokens_do_not_fit_32_bit_steps(tokens, heads):
     assert L.rekv_rotate(c.h, rotary(), SOME, heads * 64, tokens, heads, SOME, tokens, SOME, heads * 64, None) == UNSUPPORTED
     assert "too many" in c.error()
     assert L.rekv_rotate(c.h, rotary(), SOME, 64, 1, 1, SOME, 1, SOME, 64, None) == NO_GPU
+
+
+def workspace(c, tokens, seqs, max_kv, window=-1, sinks=0, prefix=0):
+    n = ctypes.c_int64(-1)
+    assert rekv.lib().rekv_attention_paged_workspace(c.h, tokens, seqs, max_kv, window, sinks, prefix, ctypes.byref(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (14, 2, 64)])
+@pytest.mark.parametrize("tokens,seqs,max_kv,prefix", [(4, 4, 20000, 5000), (64, 64, 9000, 25088), (200, 2, 30000, 4000), (1, 1, 60000, 300)])
+def test_a_prefix_has_no_window_in_the_workspace_query_either(heads, tokens, seqs, max_kv, prefix):
+    """rekv_attention_shared_prefix takes none, so a query that names one answers for the call that there is."""
+    c, L = Context(*heads), rekv.lib()
+    need = workspace(c, tokens, seqs, max_kv, prefix=prefix)
+    assert need > 0
+    cache = rekv.RekvPaged(SOME, SOME, SOME, SOME, SOME, 1000, 1000, 9000, 64, seqs, tokens)
+    for window, sinks in ((0, 0), (1, 0), (100, 30), (3000, 4)):
+        said = workspace(c, tokens, seqs, max_kv, window, sinks, prefix)
+        assert said == need
+        assert L.rekv_attention_shared_prefix(c.h, ctypes.byref(cache), SOME, SOME, prefix, max_kv, SOME, SOME, said, None) == NO_GPU
