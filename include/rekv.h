@@ -480,6 +480,11 @@ rekv_status rekv_attention_shared_prefix(rekv_ctx* ctx, const rekv_paged* cache,
 /*
  * Workspace of the two calls above, which depends on sizes alone.  Host call.  n_prefix 0: of rekv_attention_paged;
  * otherwise of rekv_attention_shared_prefix, which has no window, so window and sinks are not looked at.
+ * Smaller sizes may need more, since they are split further (28/4/128, max_kv 8,192: 4,096 tokens of 64
+ * sequences 0 bytes, 196 of one 31 MB, 64 of 64 4 MB).  One workspace for every batch of at most n_tokens
+ * tokens, whatever the rest: with R = n_tokens * Hq and S = max(2^16, min(64 R, 2^22)), 4 (D + 2) S bytes are
+ * enough for rekv_attention_paged and 4 (D + 2) (max(S, R) + max(R, min(512 R, 2^27 / (D + 2)))) for
+ * rekv_attention_shared_prefix.
  */
 rekv_status rekv_attention_paged_workspace(rekv_ctx* ctx, int32_t n_tokens, int32_t n_seqs, int32_t max_kv,
                                            int32_t window, int32_t sinks, int32_t n_prefix, int64_t* bytes);

@@ -71,3 +71,28 @@ def test_a_short_prefix_takes_one_launch():
     for heads, tokens, own, prefix in ((H7, 64, 40, 100), (H72, 64, 13, 157), (H05, 20, 1, 15), ((8, 8, 64), 5, 9, 4)):
         p = plan(heads, tokens, tokens, own, prefix=prefix)
         assert p["how"] == KEYS and p["splits"] == 1 and p["bytes"] == 0
+
+
+@pytest.mark.parametrize("dtype,heads", [(1, H7), (1, H05), (1, H72), (1, (8, 8, 64)), (1, (64, 1, 128)), (1, (5, 5, 128)), (0, (4, 1, 64)),
+                                         (0, (14, 2, 64)), (0, (6, 2, 20)), (0, (8, 8, 256))])
+def test_one_workspace_holds_every_smaller_batch(dtype, heads):
+    """The header's bound: of all batches of at most so many tokens, whatever their sequences, lengths and windows."""
+    import math
+    import random
+    rng = random.Random(7)
+    hq, _, d = heads
+
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    near = [0, 0]
+    for _ in range(4000):
+        tokens = log_int(1, 100000)
+        seqs = rng.choice([1, tokens, log_int(1, tokens), log_int(1, 5000)])
+        max_kv, window, prefix = log_int(1, 1 << 30), rng.choice([-1, -1, log_int(1, 1 << 20)]), rng.choice([0, log_int(1, 1 << 29)])
+        r = tokens * hq
+        s = max(1 << 16, min(64 * r, 1 << 22))
+        bound = 4 * (d + 2) * (s if prefix == 0 else max(s, r) + max(r, min(512 * r, (1 << 27) // (d + 2))))
+        need = plan(heads, tokens, seqs, max_kv, window if prefix == 0 else -1, 0, prefix, dtype)["bytes"]
+        assert need <= bound, (tokens, seqs, max_kv, window, prefix, need, bound)
+        near[prefix > 0] = max(near[prefix > 0], need / bound)
+    assert dtype == 0 or min(near) > 0.25, near          # and it is of their size
