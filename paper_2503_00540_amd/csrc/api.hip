@@ -799,7 +799,7 @@ static rekv_status rotary_args(rekv_ctx* c, const char* fn, const rekv_rotary* i
     }
     // the frequencies as powers of one ratio, in extended precision
     const long double ratio = powl((long double)in->base, -2.0L / d);
-    long double step = 1.0L, theta = 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
+    long double step = 1.0L, theta = 0.636619772367581343075535053490057448L;     // 2 / pi
     if (in->inverse) theta = -theta;
     for (int i = 0; i < 8; ++i, step *= ratio) r->fine[i] = (double)step;
     for (int i = 0; i * 8 < half; ++i, theta *= step) r->coarse[i] = (double)theta;

@@ -196,7 +196,7 @@ hipError_t attn_paged_launch(const PagedProblem& p, const PagedPlan& plan, int d
 // launch's arguments; with the 128 doubles themselves a call took 1.1 us more to issue.)
 constexpr int MAX_PAIRS = 128, MAX_AXES = 4;
 struct Rotary {
-    double coarse[MAX_PAIRS / 8];       // base^(-16j / D) / (2 pi), negative for the inverse
+    double coarse[MAX_PAIRS / 8];       // base^(-16j / D) * 2 / pi, quarter turns; negative for the inverse
     double fine[8];                     // base^(-2j / D)
     uint32_t axes[MAX_PAIRS / 16];      // two bits a pair
     int32_t n_axes, interleaved;        // n_axes 0: no rotation

@@ -5,8 +5,8 @@
 // Bound: HBM for many tokens (50,176 x 28 heads of 128 out of a fused projection 121 us = 5.95 TB/s, a plain copy 5.96; append of
 // 26,800 tokens at 28/4/128 with their queries 92 us = 5.4 TB/s), the launch and its round trips for few (64 users 4.8 us).  A unit of work is one 16-byte chunk of a head
 // vector and its partner half a vector on, which hold both members of their pairs in either layout.  A lane keeps one
-// chunk position of one token and walks that token's heads, so that its angles (formed in double precision, reduced to a
-// fraction of a turn) are worked out once for all of them.
+// chunk position of one token and walks that token's heads, so that its angles (formed in double precision, reduced to within
+// an eighth of a turn there) are worked out once for all of them.
 #include "common.h"
 #include "paged.h"
 
@@ -24,10 +24,12 @@ constexpr int FILL_WAVES = 4096;
 // 40,960, 153 with one per token; append of 24 streams' 26,800 tokens at 28/4/128: 93.3, 92.6, 94.5, 108.
 constexpr int MOST_WAVES[2] = {40960, 20480};
 
-// Sine and cosine of fr turns, |fr| <= 1/2: the angle less a multiple q of a quarter turn (exact) lies within pi / 4, where the Taylor
-// series to y^9 and y^10 are off by less than 2^-28; with the roundings both are within 2 units of the last place of 1.
-__device__ inline void sin_cos_turns(float fr, float* sn, float* cs) {
-    const float qf = rintf(4.f * fr), y = fmaf(qf, -0.25f, fr) * 6.283185307179586f, z = y * y;
+// Sine and cosine of t quarter turns, |t| < 2^31: the angle less a multiple q of a quarter turn (exact) lies within pi / 4, where the
+// Taylor series to y^9 and y^10 are off by less than 2^-28.  The angle is rounded to fp32 once, there, as late as it can be (2^-25 at most): with
+// the roundings of the sums both results are within 1.4 x 2^-24, rms 1.7e-8; from a fraction of a whole turn in fp32 it were 2.4 x 2^-24, rms 3.4e-8.
+__device__ inline void sin_cos_quarters(double t, float* sn, float* cs) {
+    const double qd = rint(t);
+    const float y = (float)((t - qd) * 1.5707963267948966), z = y * y;
     float s = fmaf(z, 2.7557319e-6f, -1.9841270e-4f), c = fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
     s = fmaf(z, s, 8.3333333e-3f);
     c = fmaf(z, c, -1.3888889e-3f);
@@ -35,7 +37,7 @@ __device__ inline void sin_cos_turns(float fr, float* sn, float* cs) {
     c = fmaf(z, c, 4.1666667e-2f);
     s = fmaf(z * y, s, y);
     c = fmaf(z, fmaf(z, c, -0.5f), 1.f);
-    const int q = (int)qf;
+    const int q = (int)qd;
     const float u = q & 1 ? c : s, v = q & 1 ? s : c;
     *sn = __uint_as_float(__float_as_uint(u) ^ ((uint32_t)(q & 2) << 30));
     *cs = __uint_as_float(__float_as_uint(v) ^ ((uint32_t)((q + 1) & 2) << 30));
@@ -129,7 +131,7 @@ __global__ __launch_bounds__(WAVES * 64) void rotate_kernel(RotateArgs a, int pa
             for (int e = 0; e < EPC; ++e) {
                 const uint32_t x = axes >> (2 * e) & 3;
                 const double t = (double)(x == 0 ? pos[0] : x == 1 ? pos[1] : x == 2 ? pos[2] : pos[3]) * turns[e];
-                sin_cos_turns((float)(t - rint(t)), &sn[e], &cs[e]);
+                sin_cos_quarters(t, &sn[e], &cs[e]);
             }
         }
         auto rotate = [&](u32x4& l, u32x4& r) {
