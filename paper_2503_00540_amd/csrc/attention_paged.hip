@@ -295,6 +295,16 @@ struct Rows {
         for (int db = 0; db < D / 32; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[db], pf, o[db], 0, 0, 0);
     }
 
+    // A row whose scores are all -infinity has the sum 0, and its output is 0 whatever its values are: an infinity or a NaN among them has
+    // made the products with probabilities of 0 NaN.
+    __device__ __attribute__((always_inline)) void clear_empty(float l_tot) {
+        if (l_tot != 0.f) return;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+    }
+
     // The values that drop_nonfinite took out of tiles [t0, t1), for the rows that do see them: from memory, key by key.
     __device__ __attribute__((always_inline)) void add_nonfinite(const PagedProblem& p, const Job& job, const Tiles<BN>& tiles, int t0, int t1,
                                                                  int kvh, int hh) {
@@ -497,6 +507,7 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
 
     const float l_tot = pair_sum(r.l);
     if (!r.ok) return;
+    r.clear_empty(l_tot);
     if (a.n_slots == 1) {
         const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;      // a row that sees nothing: zeros
         bf16_t* out = static_cast<bf16_t*>(p.out) + r.q_row * D + hh * 4;
@@ -592,6 +603,7 @@ __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, co
     __syncthreads();
     const int n_rows = job.n_rows - job.row0 < WM ? job.n_rows - job.row0 : WM;
     if (r.ok) {
+        r.clear_empty(l_tot);
         float m_all = ml[0][col][0];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m_all = fmaxf(m_all, ml[w][col][0]);
