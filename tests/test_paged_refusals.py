@@ -52,3 +52,20 @@ def test_a_prefix_has_no_window_in_the_workspace_query_either(heads, tokens, seq
         said = workspace(c, tokens, seqs, max_kv, window, sinks, prefix)
         assert said == need
         assert L.rekv_attention_shared_prefix(c.h, ctypes.byref(cache), SOME, SOME, prefix, max_kv, SOME, SOME, said, None) == NO_GPU
+
+
+@pytest.mark.parametrize("heads,dtype", [((14, 2, 64), rekv.REKV_BF16), ((28, 4, 128), rekv.REKV_BF16), ((4, 1, 64), rekv.REKV_F32)])
+@pytest.mark.parametrize("max_kv,prefix", [(60000, 0), (40, 5000)])
+def test_workspaces_that_are_short_missing_or_misaligned(heads, dtype, max_kv, prefix):
+    c, L = Context(*heads, dtype), rekv.lib()
+    cache = rekv.RekvPaged(SOME, SOME, SOME, SOME, SOME, 1000, 1000, 9000, 64, 2, 4)
+    need = workspace(c, 4, 2, max_kv, prefix=prefix)
+    assert need > 0
+
+    def call(p, n):
+        if prefix:
+            return L.rekv_attention_shared_prefix(c.h, ctypes.byref(cache), SOME, SOME, prefix, max_kv, SOME, p, n, None)
+        return L.rekv_attention_paged(c.h, ctypes.byref(cache), SOME, max_kv, -1, 0, SOME, p, n, None)
+    for p, n in ((None, need), (SOME, need - 1), (SOME, 0), (SOME + 16, need)):
+        assert call(p, n) == INVALID and "workspace" in c.error()
+    assert call(SOME, need) == NO_GPU
