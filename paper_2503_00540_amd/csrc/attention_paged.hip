@@ -532,7 +532,8 @@ __device__ __attribute__((always_inline)) void rows_block(const PagedArgs& a, co
 
 // A block of 32 rows, as a decode step's: its four wavefronts divide the KEYS, each walks its run of tiles through a K and a V tile
 // of its own in LDS without a barrier, and their results meet in LDS.  STREAM: non-temporal loads, where nobody else reads the keys (64
-// users' decode step 201 us so, 224 with cached loads; a live frame over 3,136 keys, which 43 blocks read, 40 and 31).
+// users' decode step 201 us so, 224 with cached loads; a live frame over 3,136 keys, which 43 blocks read, 40 and 31).  Pages below 32
+// tokens other than 16, whose rows are fetched by 64-bit addresses, have cached loads only.
 template <int D, bool TWO_PAGES, bool STREAM>
 __device__ __attribute__((always_inline)) void keys_block(const PagedArgs& a, const Job& job, int kvh, unsigned char* lds, f32x2 (*ml)[WM]) {
     typedef Source<D, TWO_PAGES, 1, STREAM> Src;
@@ -1084,8 +1085,8 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
 
 template <int D, bool TWO_PAGES>
 void launch_bf16(const PagedArgs& a, int how, dim3 grid, hipStream_t stream) {
-    if (how == STREAMED) hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, STREAMED>), grid, dim3(THREADS), 0, stream, a);
-    else if (how == KEY_BLOCKS) hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, KEY_BLOCKS>), grid, dim3(THREADS), 0, stream, a);
+    if (TWO_PAGES && how == STREAMED) hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, TWO_PAGES ? STREAMED : KEY_BLOCKS>), grid, dim3(THREADS), 0, stream, a);
+    else if (how != ROW_BLOCKS) hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, KEY_BLOCKS>), grid, dim3(THREADS), 0, stream, a);
     else hipLaunchKernelGGL((attn_paged_kernel<D, TWO_PAGES, ROW_BLOCKS>), grid, dim3(THREADS), 0, stream, a);
 }
 
