@@ -457,7 +457,10 @@ rekv_status rekv_append_kv(rekv_ctx* ctx, const rekv_paged* cache, const rekv_ro
  * more than 64 GiB are refused.
  *   q, out     [n_tokens, Hq, D]; the new tokens' keys and values are already in the pages
  *   window     tokens, the token itself among them; negative: no window (sinks is then without effect)
- *   max_kv     about the largest kv_len, for the split of the work only: any value gives right results
+ *   max_kv     about the largest kv_len, for the split of the work only: any value gives right results.  Up to
+ *              four times too large costs 0 to 25 %.  Single tokens of many users that have far less than it
+ *              says are cut into pieces most of which are empty: 64 of 28/4/128 with up to 4,096 tokens take 59 us,
+ *              69 with max_kv 32,768, 157 with 131,072 (60 MB of workspace); 480 with up to 400 48 us, 271, 997 (447 MB)
  *   workspace  device memory of at least the bytes that rekv_attention_paged_workspace gives for the same
  *              sizes, 256-byte aligned, used by this call only until it has run; may be NULL where they are 0.
  * The call allocates nothing and uses nothing of its context but the shape, so calls of one context on

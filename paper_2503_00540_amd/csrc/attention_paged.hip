@@ -13,7 +13,7 @@
 // What differs is where tiles come from: 32 keys lie in one or two pages, and the places of 64 tiles are worked out at once.
 //
 // What bounds it (28/4/128, pages of 64 to 256 unless said).  Long prompts: the matrix cores at the clock the chip grants them,
-// 1.04 to 1.07 PFLOP/s for 8,192 tokens (451 to 470 us; a library GEMM of 8,192^3 reaches 1.24), as attention_bf16.hip.  Many users' decode
+// 1.02 to 1.07 PFLOP/s for 8,192 tokens (451 to 473 us; a library GEMM of 8,192^3 reaches 1.24), as attention_bf16.hip.  Many users' decode
 // steps: HBM, 5.5 TB/s for 64 users of 1 to 8,192 tokens at 64/8/128 (199 us), 6.1 where all have 4,096.  One user's: round trips; a
 // workgroup of a 15,000-token window spends (us) 0.4 on finding its sequence, 1.3 on the page table, 0.8 to the first tile, 3.0 on two tiles
 // per wavefront and 1.2 on the merge in LDS, the joining launch 3.9, 15.7 in all.  A live frame over 3,136 keys: 0.8, 0.8 and 3.4 to the
@@ -977,9 +977,9 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     // ones half).  Blocks of 128 and of 32 rows at 28/4/128 (us): a prompt of 196 tokens 13.8 and 8.6, of 1,000 28 and 16, a live frame over
     // 3,136 at 14/2/64 22.1 and 16.8, 8 x 60 tokens over 3,000 37 and 26; the other way 32 x 16 over 3,000 36 and 44 (23 tiles a place), 8
     // x 160 through a window of 3,200 51 and 70 (26), in more than two rounds a prompt of 2,000 at 64/8/128 48 and 79, 80 x 50 tokens over 400 39 and 46.
-    // In the second round they need something to do: of 30 x 60 tokens over nothing 16 and 20, over 400 37 and 28.  On 250 random batches the
-    // choice takes 1.007 of the better time, one by tiles alone 1.054.  Beside a prefix, which larger batches have computed for all at once,
-    // SMALL is 7.
+    // In the second round they need something to do: of 30 x 60 tokens over nothing 16 and 20, over 400 37 and 28.  On the 250 random batches that
+    // it was fitted to the choice takes 1.007 of the better time, one by tiles alone 1.054; on 500 others 1.010, blocks of 32 rows always 1.013, of
+    // 128 always 1.15.  Beside a prefix, which larger batches have computed for all at once, SMALL is 7.
     const int64_t SMALL = n_prefix > 0 ? 7 : 20;
     const int64_t row_blocks = up(all_rows, BM) > n_seqs ? up(all_rows, BM) : n_seqs;
     const int64_t key_jobs = (up(all_rows, WM) > n_seqs ? up(all_rows, WM) : n_seqs) * n_kv_heads;
@@ -1022,11 +1022,14 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
     // A prefix is computed for the batch at once, by full blocks of all sequences' rows whose results are joined with the own keys', or
     // walked by each sequence's own blocks.  Measured, walked and at once (us, 28/4/128, a prefix of 4,608): 64 sequences of 12 tokens 119
     // and 77, of 24 211 and 132, of 32 228 and 158, of 48 260 and 249, of 64 280 and 305, 24 of 40 128 and 86, 16 of 12 45 and 36.  The estimate is off
-    // by a tenth where the two are alike: of these it takes the slower one at 48 and at 64 tokens.
+    // by a tenth where the two are alike: of these it takes the slower one at 48 and at 64 tokens.  On 260 random batches that it was not fitted to
+    // it takes 1.030 of the better time, at once always 1.23, walked always 1.12.
     plan.prefix_blocks = plan.prefix_splits = 0;
     plan.min_prefix_tiles = 4;
     // (fp32: lone rows walk a prefix of up to F32_SHORT tiles, and up to F32_WHOLE tiles are not split.  30 users' tokens after five tiles at
-    // 14/2/64 take 10.5 us at once, 9.5 walked in two splits, 8.0 in one; after 13 tiles 11.1, 11.1 and 13.1; after 32 11.1 and 15.2.)
+    // 14/2/64 take 10.5 us at once, 9.5 walked in two splits, 8.0 in one; after 13 tiles 11.1, 11.1 and 13.1; after 32 11.1 and 15.2.  Users of eight
+    // rows or more walk every prefix, which long ones make dear: 8 users of 28/4/128 with 13 tokens after 4,000 take 39 us, 26 at once.  The splits of a
+    // prefix at once come from the estimate for bf16 blocks; on 81 batches they take 1.031 of the best power of two's time, 1.20 at worst.)
     constexpr int64_t F32_SHORT = 16, F32_WHOLE = 8;
     bool together = !bf16 && all_rows < n_seqs * (F32_ROWS / 2) && n_prefix > F32_SHORT * BN;
     const int64_t prefix_rows = bf16 ? BM : F32_ROWS, prefix_tiles = up(n_prefix, BN);
@@ -1047,7 +1050,7 @@ PagedPlan attn_paged_plan(int dtype, int n_q_heads, int n_kv_heads, int head_dim
             }
         }
         if (bf16 && lone) {
-            // (of 125 random batches 1.015 of the better time; all at once 1.26, all walked 1.08)
+            // (of the 125 random batches it was fitted to 1.015 of the better time, all at once 1.26, all walked 1.08; of 260 others 1.023, 1.13, 1.14)
             const double own = few_us(up(keys, BN), 0, true, &few_splits);
             together = (best > own ? best : own) + slot_us + 1.0 < few_us(up(keys + n_prefix, BN), n_prefix, false, &few_splits);
         } else if (!together) {

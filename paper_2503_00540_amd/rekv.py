@@ -678,7 +678,8 @@ class Rekv:
                         window: int | None = None, sinks: int = 0, out=None):
         """rekv_attention_paged: q [n_tokens, Hq, D] of a ragged batch over the pages [n_pages, page_size, Hkv, D].  window None: all
         keys; otherwise the last `window` of them, the token itself among them, and the first `sinks`.  max_kv: about the
-        largest kv_len (None: what the table holds), for the split of the work only."""
+        largest kv_len, for the split of the work only.  None: what the table holds, which is slow where many users' tables are far
+        wider than their sequences (rekv.h has figures); a bound that a scheduler or a captured step has is better."""
         done = self._fast.attention_paged(q, k_pages, v_pages, token_start, kv_len, page_table, max_kv, window, sinks, out)
         if done is not None:
             return done
